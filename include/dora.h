@@ -68,7 +68,10 @@ typedef enum {
     DORA_PHASE_BACKWARD_RECOMPUTE = 3,/* dora_backward with saved_* == NULL (recomputes h and inner) */
     DORA_PHASE_COMPOSE_BACKWARD = 4,  /* dora_compose_backward */
     DORA_PHASE_FORWARD_DROPOUT = 5,   /* dora_forward_dropout, worst case as for DORA_PHASE_FORWARD */
-    DORA_PHASE_BACKWARD_DROPOUT = 6   /* dora_backward_dropout with everything recomputed (worst case) */
+    DORA_PHASE_BACKWARD_DROPOUT = 6,  /* dora_backward_dropout with everything recomputed (worst case) */
+    DORA_PHASE_NORM_QUANT = 7,        /* dora_norm_quant */
+    DORA_PHASE_FORWARD_QUANT = 8,     /* dora_forward_quant, worst case, an input of the adapter's own among it */
+    DORA_PHASE_BACKWARD_QUANT = 9     /* dora_backward_quant, the same */
 } dora_phase;
 
 /* Scratch bytes an entry point needs for this shape.  Returns 0 for an invalid desc. */
@@ -255,6 +258,82 @@ dora_status dora_backward_dropout(const dora_desc* desc, const void* dy, const v
                                   const void* A, const void* B, const float* m, const float* w_norm,
                                   const void* saved_h, const void* saved_inner, void* dx, void* dx_lora,
                                   float* dA, float* dB, float* dm, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Frozen weights in 4 bits: codes and one scale per `group` consecutive weights of a row,
+ *   W[j,k] = scale[j, k / group] * v(q[j,k])
+ *   DORA_QUANT_INT4 : v(q) = q - zero, the unsigned code less a zero point: zero[j, k / group], or 8 where zero is NULL.
+ *   DORA_QUANT_FP4  : v(q) the E2M1 float q (sign, two bits of exponent, one of mantissa: 0, .5, 1, 1.5, 2, 3, 4, 6);
+ *                     zero must be NULL.
+ *   q           : device, [d_out, d_in / 2] bytes, row-major; byte i of a row holds weight 2 i in its low and 2 i + 1 in
+ *                 its high four bits.
+ *   scale, zero : device, the desc's `dtype`, [d_out, ceil(d_in / group)], any finite values.
+ *   group       : a power of two, 32 at least; the last group of a row may be short.
+ * d_in is a multiple of 8 for every dtype.  The struct is read by the call and need not outlive it.  A bad code, group or zero
+ * is DORA_ERR_SHAPE.
+ */
+typedef enum { DORA_QUANT_INT4 = 0, DORA_QUANT_FP4 = 1 } dora_quant_code;
+typedef struct {
+    int32_t code;   /* dora_quant_code */
+    int32_t group;
+    const void* q;
+    const void* scale;
+    const void* zero;
+} dora_quant;
+
+/*
+ * dora_quantize   : codes, scales and (INT4, zero != NULL) zero points of W [d_out, d_in] `dtype`, rounded to nearest.
+ *     INT4, zero == NULL : scale = max|w| / 7, q = 8 + round(w / scale).
+ *     INT4 with zero     : over the group and 0, scale = (max - min) / 15, zero = round(-min / scale), q = zero + round(w / scale).
+ *     FP4                : scale = max|w| / 6, q the nearest E2M1 float to w / scale, halfway to the even code.
+ *   Scales are rounded to four significant bits (to nearest; with a zero point upwards), so that a weight read back is a
+ *   bf16 or fp16 number without rounding.  Codes are kept in range, in fp16 also so that no weight reads back as an infinity; a group whose scale is 0 reads back as 0, one that
+ *   holds an infinity or NaN has scale NaN and reads back as NaN.
+ * dora_dequantize : W [d_out, d_in] `dtype` out, rounded once.
+ * r and tokens of desc are not read.  Neither needs a workspace.
+ */
+dora_status dora_quantize(const dora_desc* desc, const void* W, int code, int group, void* q, void* scale, void* zero, void* stream);
+dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W, void* stream);
+
+/*
+ * The module over such a weight: dora_norm, dora_forward(_dropout) and dora_backward(_dropout) with `wq` in the place of W,
+ * arguments and results as there.
+ *   x_lora : the adapter's own input as in dora_forward_dropout / dora_backward_dropout, or NULL: the plain module (as in
+ *            the forward x itself).  In dora_backward_quant with x_lora, x is not read and may be NULL, and dx_lora receives
+ *            the gradient of the adapter's input; without it dx_lora is not written.
+ * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  The routes that multiply tiles
+ * read W back into the workspace in the storage type first (2 or 4 bytes a weight), rounded once, which scales of up to four
+ * significant bits and zero points of 0 to 15 do not show.
+ */
+dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const void* A, const void* B, float* w_norm, void* ws,
+                            size_t ws_bytes, void* stream);
+dora_status dora_forward_quant(const dora_desc* desc, const void* x, const void* x_lora, const dora_quant* wq, const void* A,
+                               const void* B, const float* m, const float* w_norm, const void* bias, void* y, void* saved_h,
+                               void* saved_inner, float* w_norm_out, void* ws, size_t ws_bytes, void* stream);
+dora_status dora_backward_quant(const dora_desc* desc, const void* dy, const void* x, const void* x_lora, const dora_quant* wq,
+                                const void* A, const void* B, const float* m, const float* w_norm, const void* saved_h,
+                                const void* saved_inner, void* dx, void* dx_lora, float* dA, float* dB, float* dm, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/*
+ * The dropout in front of the adapter, for the x_lora of the calls above.  The mask is never stored: it is a function of seed,
+ * offset and place, and the same arguments give the same mask again in the backward or a recomputed forward, for any dtype.
+ *   dora_dropout          : x_lora = keep (.) x / (1 - p)             x, x_lora [tokens, d_in] `dtype`; x_lora may be x
+ *   dora_dropout_backward : dx_sum = dx + keep (.) dx_lora / (1 - p)  all [tokens, d_in] `dtype`, fp32 sum, rounded once;
+ *                           dx == NULL counts as 0; dx_sum may be dx or dx_lora
+ * Elements are numbered along the rows from 0; eight of them share a block.  Block b takes the 128 bits of Philox 4x32-10 under key
+ * `seed` at the counter whose low 64 bits are offset + *counter + b (mod 2^64) and whose high ones are 0; bits 16 j .. 16 j + 15
+ * decide element j, which is dropped where they are below round(65536 p) (at most 65535): p is used to the nearest 2^-16, and 1 - p
+ * is that of the p used.  A call draws ceil(tokens d_in / 8) blocks; rows from t on (t d_in a multiple of 8) are reached by an
+ * offset of t d_in / 8.
+ *   p : 0 <= p < 1 (DORA_ERR_SHAPE otherwise).   counter : device, one uint64, or NULL (0): read when the launch runs, so
+ *   that a captured graph draws anew in every replay.
+ * What is dropped does not reach the result (NaN and infinities included).  d_out and r of desc are not read.  No workspace.
+ */
+dora_status dora_dropout(const dora_desc* desc, const void* x, double p, uint64_t seed, uint64_t offset, const uint64_t* counter,
+                         void* x_lora, void* stream);
+dora_status dora_dropout_backward(const dora_desc* desc, const void* dx_lora, double p, uint64_t seed, uint64_t offset,
+                                  const uint64_t* counter, const void* dx, void* dx_sum, void* stream);
 
 const char* dora_status_str(int status);
 

@@ -44,7 +44,10 @@ enum {
     DORA_K_PROBE_MFMA = 17,  /* dora_probe_mfma                                        */
     DORA_K_GEMM_FUSED_FWD = 18, /* y = g (.) ([x | s*h] [W | B]^T); y of a few tokens    */
     DORA_K_SPLITK_REDUCE = 19,  /* fixed-order sum of the K slices of a short product     */
-    DORA_K_COUNT = 20
+    DORA_K_QUANTIZE = 20,    /* dora_quantize                                          */
+    DORA_K_DEQUANTIZE = 21,  /* 4-bit weight to storage: dora_dequantize, tiled routes */
+    DORA_K_DROPOUT = 22,     /* dora_dropout, dora_dropout_backward                    */
+    DORA_K_COUNT = 23
 };
 void dora_trace_enable(int on);
 void dora_trace_select(uint64_t kernel_mask); /* bit k set = bracket launches of kernel id k (default: all) */

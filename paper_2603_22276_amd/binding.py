@@ -15,12 +15,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdora.so")
 
 DORA_F32, DORA_BF16, DORA_F16 = 0, 1, 2
-PHASE_NORM, PHASE_FORWARD, PHASE_BACKWARD, PHASE_BACKWARD_RECOMPUTE, PHASE_COMPOSE_BACKWARD, PHASE_FORWARD_DROPOUT, PHASE_BACKWARD_DROPOUT = range(7)
-K_COUNT = 20
+PHASE_NORM, PHASE_FORWARD, PHASE_BACKWARD, PHASE_BACKWARD_RECOMPUTE, PHASE_COMPOSE_BACKWARD, PHASE_FORWARD_DROPOUT, PHASE_BACKWARD_DROPOUT, PHASE_NORM_QUANT, PHASE_FORWARD_QUANT, PHASE_BACKWARD_QUANT = range(10)
+QUANT_INT4, QUANT_FP4 = 0, 1
+K_COUNT = 23
 
 EXPORTS = (
     "dora_workspace_bytes", "dora_norm", "dora_norm_static", "dora_norm_static_max_bytes", "dora_base_sq", "dora_norm_cached", "dora_norm_terms", "dora_norm_assemble", "dora_mag_scale", "dora_compose", "dora_compose_backward",
     "dora_project", "dora_forward", "dora_forward_fused", "dora_backward", "dora_forward_dropout", "dora_backward_dropout", "dora_status_str",
+    "dora_quantize", "dora_dequantize", "dora_norm_quant", "dora_forward_quant", "dora_backward_quant", "dora_dropout", "dora_dropout_backward",
     "dora_probe_copy", "dora_probe_mfma",
     "dora_trace_enable", "dora_trace_select", "dora_trace_reset", "dora_trace_collect", "dora_trace_get", "dora_trace_name",
 )
@@ -37,6 +39,10 @@ class dora_desc(ctypes.Structure):
         ("d_out", ctypes.c_int64), ("d_in", ctypes.c_int64), ("r", ctypes.c_int64), ("tokens", ctypes.c_int64),
         ("dtype", ctypes.c_int32), ("s", ctypes.c_float), ("eps", ctypes.c_float),
     ]
+
+
+class dora_quant(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_int32), ("group", ctypes.c_int32), ("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("zero", ctypes.c_void_p)]
 
 
 _lib = None
@@ -70,10 +76,19 @@ def lib() -> ctypes.CDLL:
         L.dora_backward.argtypes = [dp, vp, vp, vp, vp, vp, fp, fp, vp, vp, vp, fp, fp, fp, vp, sz, vp]
         L.dora_forward_dropout.argtypes = [dp, vp, vp, vp, vp, vp, fp, fp, vp, vp, vp, vp, fp, vp, sz, vp]
         L.dora_backward_dropout.argtypes = [dp, vp, vp, vp, vp, vp, fp, fp, vp, vp, vp, vp, fp, fp, fp, vp, sz, vp]
+        qp, u64, f64 = ctypes.POINTER(dora_quant), ctypes.c_uint64, ctypes.c_double
+        L.dora_quantize.argtypes = [dp, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp, vp]
+        L.dora_dequantize.argtypes = [dp, qp, vp, vp]
+        L.dora_norm_quant.argtypes = [dp, qp, vp, vp, fp, vp, sz, vp]
+        L.dora_forward_quant.argtypes = [dp, vp, vp, qp, vp, vp, fp, fp, vp, vp, vp, vp, fp, vp, sz, vp]
+        L.dora_backward_quant.argtypes = [dp, vp, vp, vp, qp, vp, vp, fp, fp, vp, vp, vp, vp, fp, fp, fp, vp, sz, vp]
+        L.dora_dropout.argtypes = [dp, vp, f64, u64, u64, vp, vp, vp]
+        L.dora_dropout_backward.argtypes = [dp, vp, f64, u64, u64, vp, vp, vp, vp]
         L.dora_probe_copy.argtypes = [vp, vp, sz, vp]
         L.dora_probe_mfma.argtypes = [vp, fp, ctypes.c_int, ctypes.c_int, vp]
         for f in (L.dora_probe_copy, L.dora_probe_mfma, L.dora_norm, L.dora_norm_static, L.dora_base_sq, L.dora_norm_cached, L.dora_norm_terms, L.dora_norm_assemble, L.dora_mag_scale, L.dora_compose, L.dora_compose_backward, L.dora_project, L.dora_forward, L.dora_forward_fused,
-                  L.dora_backward, L.dora_forward_dropout, L.dora_backward_dropout, L.dora_trace_collect, L.dora_trace_get):
+                  L.dora_backward, L.dora_forward_dropout, L.dora_backward_dropout, L.dora_quantize, L.dora_dequantize, L.dora_norm_quant, L.dora_forward_quant,
+                  L.dora_backward_quant, L.dora_dropout, L.dora_dropout_backward, L.dora_trace_collect, L.dora_trace_get):
             f.restype = ctypes.c_int
         L.dora_status_str.argtypes = [ctypes.c_int]
         L.dora_status_str.restype = ctypes.c_char_p
@@ -97,6 +112,13 @@ def status_str(status: int) -> str:
 
 def make_desc(d_out: int, d_in: int, r: int, tokens: int, dtype: int, s: float, eps: float = 0.0) -> dora_desc:
     return dora_desc(int(d_out), int(d_in), int(r), int(tokens), int(dtype), float(s), float(eps))
+
+
+def make_quant(code: int, group: int, q, scale, zero=None) -> dora_quant:
+    """A 4-bit weight from its tensors (or raw addresses); the struct keeps them alive."""
+    w = dora_quant(int(code), int(group), _p(q), _p(scale), _p(zero))
+    w.tensors = (q, scale, zero)
+    return w
 
 
 def _p(t) -> Optional[int]:
@@ -212,6 +234,42 @@ def dora_backward_dropout(desc, dy, x_lora, W, A, B, m, w_norm, saved_h, saved_i
     _check(lib().dora_backward_dropout(ctypes.byref(desc), _p(dy), _p(x_lora), _p(W), _p(A), _p(B), _p(m), _p(w_norm),
                                        _p(saved_h), _p(saved_inner), _p(dx), _p(dx_lora), _p(dA), _p(dB), _p(dm), _p(ws),
                                        _nbytes(ws), _stream(stream)), "dora_backward_dropout")
+
+
+def dora_quantize(desc, W, code: int, group: int, q, scale, zero, stream=None) -> None:
+    _check(lib().dora_quantize(ctypes.byref(desc), _p(W), int(code), int(group), _p(q), _p(scale), _p(zero), _stream(stream)),
+           "dora_quantize")
+
+
+def dora_dequantize(desc, wq, W, stream=None) -> None:
+    _check(lib().dora_dequantize(ctypes.byref(desc), ctypes.byref(wq), _p(W), _stream(stream)), "dora_dequantize")
+
+
+def dora_norm_quant(desc, wq, A, B, w_norm, ws, stream=None) -> None:
+    _check(lib().dora_norm_quant(ctypes.byref(desc), ctypes.byref(wq), _p(A), _p(B), _p(w_norm), _p(ws), _nbytes(ws), _stream(stream)),
+           "dora_norm_quant")
+
+
+def dora_forward_quant(desc, x, x_lora, wq, A, B, m, w_norm, bias, y, saved_h, saved_inner, w_norm_out, ws, stream=None) -> None:
+    _check(lib().dora_forward_quant(ctypes.byref(desc), _p(x), _p(x_lora), ctypes.byref(wq), _p(A), _p(B), _p(m), _p(w_norm), _p(bias),
+                                    _p(y), _p(saved_h), _p(saved_inner), _p(w_norm_out), _p(ws), _nbytes(ws), _stream(stream)),
+           "dora_forward_quant")
+
+
+def dora_backward_quant(desc, dy, x, x_lora, wq, A, B, m, w_norm, saved_h, saved_inner, dx, dx_lora, dA, dB, dm, ws, stream=None) -> None:
+    _check(lib().dora_backward_quant(ctypes.byref(desc), _p(dy), _p(x), _p(x_lora), ctypes.byref(wq), _p(A), _p(B), _p(m), _p(w_norm),
+                                     _p(saved_h), _p(saved_inner), _p(dx), _p(dx_lora), _p(dA), _p(dB), _p(dm), _p(ws), _nbytes(ws),
+                                     _stream(stream)), "dora_backward_quant")
+
+
+def dora_dropout(desc, x, p: float, seed: int, offset: int, counter, x_lora, stream=None) -> None:
+    _check(lib().dora_dropout(ctypes.byref(desc), _p(x), float(p), int(seed), int(offset), _p(counter), _p(x_lora), _stream(stream)),
+           "dora_dropout")
+
+
+def dora_dropout_backward(desc, dx_lora, p: float, seed: int, offset: int, counter, dx, dx_sum, stream=None) -> None:
+    _check(lib().dora_dropout_backward(ctypes.byref(desc), _p(dx_lora), float(p), int(seed), int(offset), _p(counter), _p(dx), _p(dx_sum),
+                                       _stream(stream)), "dora_dropout_backward")
 
 
 def dora_probe_copy(src, dst, nbytes: int, stream=None) -> None:

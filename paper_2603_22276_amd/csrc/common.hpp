@@ -333,6 +333,30 @@ hipError_t launch_splitk_reduce(const float* partials, int ksplit, int64_t n, in
                                 hipStream_t st, const float* colscale = nullptr, const void* colbias = nullptr, int cols = 0,
                                 Waiting* waiting = nullptr);
 
+// ---- 4-bit frozen weights (quant.hip) --------------------------------------------------------------
+struct QuantWeight {          // a dora_quant and its shape
+    const uint32_t* q;        // [d_out][d_in / 8]
+    const void *scale, *zero; // [d_out][groups]; zero may be nullptr
+    int code, group_shift, groups;
+    int d_out, d_in;
+};
+inline int quant_groups(int d_in, int group_shift) { return (int)(((int64_t)d_in + ((int64_t)1 << group_shift) - 1) >> group_shift); }
+hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int code, int group_shift, void* q, void* scale, void* zero,
+                           hipStream_t st);
+hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st);
+
+// ---- dropout with a mask that is drawn where it is needed (dropout.hip) -----------------------------
+struct DropoutArgs {
+    const void *v, *add;      // add may be nullptr
+    void* out;
+    int64_t n;
+    uint64_t seed, offset;
+    const uint64_t* counter;  // device, added to offset, or nullptr
+    uint32_t threshold;       // of 65536: below it an element is dropped
+    float scale;
+};
+hipError_t launch_dropout(int dtype, const DropoutArgs& a, hipStream_t st);
+
 hipError_t launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream_t st);
 hipError_t launch_mfma_probe(const void* operands, float* sink, int iters, int workgroups, hipStream_t st);
 

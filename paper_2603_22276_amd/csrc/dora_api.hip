@@ -145,6 +145,30 @@ struct Bump {
 constexpr int TILE = 128;
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// A 4-bit weight's struct against the desc's shape (d_out and d_in only)
+dora_status check_quant_shape(const dora_desc* d, int code, int group, const void* zero)
+{
+    const dora_status st = check_desc(d, false);
+    if (st != DORA_OK) return st;
+    if (d->d_in < 8 || d->d_in % 8 || d->d_out * d->d_in >= MAX_ELEMS) return DORA_ERR_SHAPE;
+    if (code != DORA_QUANT_INT4 && code != DORA_QUANT_FP4) return DORA_ERR_SHAPE;
+    if (group < 32 || (group & (group - 1))) return DORA_ERR_SHAPE;
+    if (code == DORA_QUANT_FP4 && zero) return DORA_ERR_SHAPE;
+    return DORA_OK;
+}
+dora_status check_quant(const dora_desc* d, const dora_quant* wq, QuantWeight& w)
+{
+    if (!wq) return DORA_ERR_NULL;
+    const dora_status st = check_quant_shape(d, wq->code, wq->group, wq->zero);
+    if (st != DORA_OK) return st;
+    DORA_REQ_PTR(wq->q); DORA_REQ_PTR(wq->scale); DORA_OPT_PTR(wq->zero);
+    const int shift = __builtin_ctz((unsigned)wq->group);
+    w = QuantWeight{(const uint32_t*)wq->q, wq->scale, wq->zero, wq->code, shift, quant_groups((int)d->d_in, shift), (int)d->d_out, (int)d->d_in};
+    return DORA_OK;
+}
+// scratch for such a weight in the storage type
+inline void* take_weight(const dora_desc* d, Bump& b) { return b.take_bytes((size_t)d->d_out * d->d_in * esize(d->dtype)); }
+
 struct NormPlan {
     int tiles_n;   // N tiles of the [d_out, r] row-dot contractions
     int ks_u;      // split of d_in for U = W A^T
@@ -367,6 +391,8 @@ hipError_t contract(int dtype, bool a_kc, bool b_kc, int M, int N, const Seg* se
 // c == nullptr: only the terms are wanted.  terms != nullptr: [3, d_out] fp32 receives base_sq, cross, ba_sq.
 // G_out != nullptr: [r, r] fp32 receives the Gram matrix of Eq. 4.
 // waiting != nullptr: the last launch may be left there.
+// G is an operand of the B G product (16-bit): a rank whose Gram matrix cannot be one
+inline bool norm_refused(const dora_desc* d) { return is16(d->dtype) && d->s != 0.f && d->r * d->r >= MAX_ELEMS; }
 // Eq. 6 riding on the norm's last launch: set `done` when g / gm1 were written there
 struct MagOut { const float* m; float eps; float* g; float* gm1; bool done; };
 
@@ -392,7 +418,7 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
         return DORA_OK;
     }
     if (is16(d->dtype)) {
-        if ((int64_t)r * r >= MAX_ELEMS) return DORA_ERR_SHAPE;   // G is an operand of the B G product
+        if (norm_refused(d)) return DORA_ERR_SHAPE;
         const int dt = dt_of(d->dtype);
         // past that rank B no longer fits the registers of a workgroup
         if (r <= NORM_ROWS_MAX_RANK) {
@@ -639,6 +665,7 @@ size_t dora_workspace_bytes(const dora_desc* desc, int phase)
         return n > 0 ? n : 256;   // 0 is reserved for "invalid desc"
     }
     if (check_desc(desc, true) != DORA_OK) return 0;
+    if (phase >= DORA_PHASE_NORM_QUANT && desc->d_in % 8) return 0;
     Bump b(nullptr);
     switch (phase) {
         case DORA_PHASE_NORM: { NormPlan n; plan_norm(desc, b, n); break; }
@@ -647,6 +674,9 @@ size_t dora_workspace_bytes(const dora_desc* desc, int phase)
         case DORA_PHASE_BACKWARD_RECOMPUTE: { BwdPlan p; plan_bwd(desc, b, p, true, true, true); break; }
         case DORA_PHASE_FORWARD_DROPOUT: { FwdPlan p; plan_fwd(desc, b, p, true, true, true, true, true); break; }
         case DORA_PHASE_BACKWARD_DROPOUT: { BwdPlan p; plan_bwd(desc, b, p, true, true, true, true); break; }
+        case DORA_PHASE_NORM_QUANT: { NormPlan n; take_weight(desc, b); plan_norm(desc, b, n); break; }
+        case DORA_PHASE_FORWARD_QUANT: { FwdPlan p; take_weight(desc, b); plan_fwd(desc, b, p, true, true, true, true, true); break; }
+        case DORA_PHASE_BACKWARD_QUANT: { BwdPlan p; take_weight(desc, b); plan_bwd(desc, b, p, true, true, true, true); break; }
         default: return 0;
     }
     return b.off > 0 ? b.off : 256;
@@ -811,14 +841,16 @@ static GemmArgs inner_product(const dora_desc* d, const void* x, const void* W, 
 }
 
 // one_product: the K-concatenated forward (h, then [x | s h] [W | B]^T with the compose in its epilogue), else x W^T,
-// h B^T and a compose pass over both.
+// h B^T and a compose pass over both.  wq != nullptr: W in 4 bits, read back into the workspace first.
 static dora_status forward_impl(const dora_desc* desc, const void* x, const void* x_lora, const void* W, const void* A,
                                 const void* B, const float* m, const float* w_norm, const void* bias, void* y, void* saved_h,
-                                void* saved_inner, float* w_norm_out, void* ws, size_t ws_bytes, void* stream, bool one_product)
+                                void* saved_inner, float* w_norm_out, void* ws, size_t ws_bytes, void* stream, bool one_product,
+                                const QuantWeight* wq = nullptr)
 {
     dora_status st = check_desc(desc, true);
     if (st != DORA_OK) return st;
-    DORA_REQ_PTR(W); DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(m);
+    if (!wq) DORA_REQ_PTR(W);
+    DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(m);
     if (desc->tokens > 0) { DORA_REQ_PTR(x); DORA_REQ_PTR(y); }
     DORA_OPT_PTR(x_lora);
     DORA_OPT_PTR(w_norm); DORA_OPT_PTR(bias); DORA_OPT_PTR(saved_h); DORA_OPT_PTR(saved_inner); DORA_OPT_PTR(w_norm_out);
@@ -826,13 +858,21 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     const bool dropout = (x_lora != nullptr);
     const bool f32_plain = desc->dtype == DORA_F32 && !dropout;
     const bool need_lora = !one_product && !f32_plain && saved_inner == nullptr;
+    const bool need_weight = wq && (need_norm || desc->tokens > 0);
+    if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     FwdPlan p;
+    if (need_weight) take_weight(desc, sizing);
     plan_fwd(desc, sizing, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout);
     if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
     Bump b(ws);
-    plan_fwd(desc, b, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout);
     hipStream_t s = (hipStream_t)stream;
+    if (need_weight) {
+        void* const read_back = take_weight(desc, b);
+        DORA_HIP(launch_dequantize(desc->dtype, *wq, read_back, s));
+        W = read_back;
+    }
+    plan_fwd(desc, b, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout);
     const int T = (int)desc->tokens, d_out = (int)desc->d_out, d_in = (int)desc->d_in, r = (int)desc->r;
 
     float* const gm1 = one_product ? nullptr : p.gm1;   // only the compose pass reads g - 1
@@ -988,13 +1028,14 @@ static dora_status backward_f32(const dora_desc* d, const void* dy, const void* 
 static dora_status backward_impl(const dora_desc* desc, const void* dy, const void* x, const void* x_lora, const void* W,
                                  const void* A, const void* B, const float* m, const float* w_norm, const void* saved_h,
                                  const void* saved_inner, void* dx, void* dx_lora, float* dA, float* dB, float* dm,
-                                 void* ws, size_t ws_bytes, void* stream)
+                                 void* ws, size_t ws_bytes, void* stream, const QuantWeight* wq = nullptr)
 {
     dora_status st = check_desc(desc, true);
     if (st != DORA_OK) return st;
     const bool dropout = (x_lora != nullptr);
     const void* xa = dropout ? x_lora : x;
-    DORA_REQ_PTR(W); DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(m);
+    if (!wq) DORA_REQ_PTR(W);
+    DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(m);
     if (desc->tokens > 0) { DORA_REQ_PTR(dy); DORA_REQ_PTR(xa); }
     DORA_OPT_PTR(w_norm); DORA_OPT_PTR(saved_h); DORA_OPT_PTR(saved_inner);
     DORA_OPT_PTR(dx); DORA_OPT_PTR(dx_lora); DORA_OPT_PTR(dA); DORA_OPT_PTR(dB); DORA_OPT_PTR(dm);
@@ -1002,13 +1043,21 @@ static dora_status backward_impl(const dora_desc* desc, const void* dy, const vo
     const bool need_inner = (dm != nullptr) && (saved_inner == nullptr);
     const bool need_h = (saved_h == nullptr) && (dB != nullptr || need_inner);
     const bool need_dzb = dropout && (dx_lora != nullptr);
+    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && (need_inner || dx || need_dzb)));
+    if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     BwdPlan p;
+    if (need_weight) take_weight(desc, sizing);
     plan_bwd(desc, sizing, p, need_norm, need_h, need_inner, need_dzb);
     if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
     Bump b(ws);
-    plan_bwd(desc, b, p, need_norm, need_h, need_inner, need_dzb);
     hipStream_t s = (hipStream_t)stream;
+    if (need_weight) {
+        void* const read_back = take_weight(desc, b);
+        DORA_HIP(launch_dequantize(desc->dtype, *wq, read_back, s));
+        W = read_back;
+    }
+    plan_bwd(desc, b, p, need_norm, need_h, need_inner, need_dzb);
     const int T = (int)desc->tokens, d_out = (int)desc->d_out, d_in = (int)desc->d_in, r = (int)desc->r;
     const int dt = desc->dtype;
 
@@ -1153,6 +1202,104 @@ dora_status dora_backward_dropout(const dora_desc* desc, const void* dy, const v
                          ws_bytes, stream);
 }
 
+dora_status dora_quantize(const dora_desc* desc, const void* W, int code, int group, void* q, void* scale, void* zero, void* stream)
+{
+    const dora_status st = check_quant_shape(desc, code, group, zero);
+    if (st != DORA_OK) return st;
+    DORA_REQ_PTR(W); DORA_REQ_PTR(q); DORA_REQ_PTR(scale); DORA_OPT_PTR(zero);
+    DORA_HIP(launch_quantize(desc->dtype, W, (int)desc->d_out, (int)desc->d_in, code, __builtin_ctz((unsigned)group), q, scale, zero,
+                             (hipStream_t)stream));
+    return DORA_OK;
+}
+
+dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W, void* stream)
+{
+    QuantWeight w;
+    const dora_status st = check_quant(desc, wq, w);
+    if (st != DORA_OK) return st;
+    DORA_REQ_PTR(W);
+    DORA_HIP(launch_dequantize(desc->dtype, w, W, (hipStream_t)stream));
+    return DORA_OK;
+}
+
+dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const void* A, const void* B, float* w_norm, void* ws,
+                            size_t ws_bytes, void* stream)
+{
+    QuantWeight w;
+    dora_status st = check_desc(desc, true);
+    if (st != DORA_OK || (st = check_quant(desc, wq, w)) != DORA_OK) return st;
+    DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(w_norm);
+    if (norm_refused(desc)) return DORA_ERR_SHAPE;
+    Bump sizing(nullptr);
+    NormPlan n;
+    take_weight(desc, sizing);
+    plan_norm(desc, sizing, n);
+    if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
+    Bump b(ws);
+    void* const W = take_weight(desc, b);
+    plan_norm(desc, b, n);
+    DORA_HIP(launch_dequantize(desc->dtype, w, W, (hipStream_t)stream));
+    return norm_impl(desc, W, A, B, w_norm, n, (hipStream_t)stream);
+}
+
+dora_status dora_forward_quant(const dora_desc* desc, const void* x, const void* x_lora, const dora_quant* wq, const void* A,
+                               const void* B, const float* m, const float* w_norm, const void* bias, void* y, void* saved_h,
+                               void* saved_inner, float* w_norm_out, void* ws, size_t ws_bytes, void* stream)
+{
+    QuantWeight w;
+    dora_status st = check_desc(desc, true);
+    if (st != DORA_OK || (st = check_quant(desc, wq, w)) != DORA_OK) return st;
+    if (x_lora == x || desc->tokens == 0) x_lora = nullptr;
+    return forward_impl(desc, x, x_lora, nullptr, A, B, m, w_norm, bias, y, saved_h, saved_inner, w_norm_out, ws, ws_bytes, stream,
+                        !x_lora && forward_in_one_product(desc), &w);
+}
+
+dora_status dora_backward_quant(const dora_desc* desc, const void* dy, const void* x, const void* x_lora, const dora_quant* wq,
+                                const void* A, const void* B, const float* m, const float* w_norm, const void* saved_h,
+                                const void* saved_inner, void* dx, void* dx_lora, float* dA, float* dB, float* dm, void* ws,
+                                size_t ws_bytes, void* stream)
+{
+    QuantWeight w;
+    dora_status st = check_desc(desc, true);
+    if (st != DORA_OK || (st = check_quant(desc, wq, w)) != DORA_OK) return st;
+    if (x_lora) x = nullptr;
+    else dx_lora = nullptr;
+    return backward_impl(desc, dy, x, x_lora, nullptr, A, B, m, w_norm, saved_h, saved_inner, dx, dx_lora, dA, dB, dm, ws, ws_bytes,
+                         stream, &w);
+}
+
+// v (x or dx_lora) under the mask, added to `add` where that is given
+static dora_status dropout_impl(const dora_desc* d, const void* v, double p, uint64_t seed, uint64_t offset, const uint64_t* counter,
+                                const void* add, void* out, void* stream)
+{
+    if (!d) return DORA_ERR_NULL;
+    if (d->dtype != DORA_F32 && d->dtype != DORA_BF16 && d->dtype != DORA_F16) return DORA_ERR_DTYPE;
+    const int64_t mult = is16(d->dtype) ? 8 : 4;
+    if (d->d_in < mult || d->d_in % mult || d->d_in >= MAX_ELEMS || d->tokens < 0 || d->tokens >= MAX_ELEMS || d->tokens * d->d_in >= MAX_ELEMS)
+        return DORA_ERR_SHAPE;
+    if (!(p >= 0.0 && p < 1.0)) return DORA_ERR_SHAPE;
+    if (d->tokens > 0) { DORA_REQ_PTR(v); DORA_REQ_PTR(out); }
+    DORA_OPT_PTR(add);
+    if (counter && !aligned(counter, 8)) return DORA_ERR_ALIGN;
+    if (d->tokens == 0) return DORA_OK;
+    const uint32_t t = (uint32_t)std::min(65535l, lrint(p * 65536.0));
+    DORA_HIP(launch_dropout(d->dtype, DropoutArgs{v, add, out, d->tokens * d->d_in, seed, offset, counter, t, (float)(65536.0 / (65536 - t))},
+                            (hipStream_t)stream));
+    return DORA_OK;
+}
+
+dora_status dora_dropout(const dora_desc* desc, const void* x, double p, uint64_t seed, uint64_t offset, const uint64_t* counter,
+                         void* x_lora, void* stream)
+{
+    return dropout_impl(desc, x, p, seed, offset, counter, nullptr, x_lora, stream);
+}
+
+dora_status dora_dropout_backward(const dora_desc* desc, const void* dx_lora, double p, uint64_t seed, uint64_t offset,
+                                  const uint64_t* counter, const void* dx, void* dx_sum, void* stream)
+{
+    return dropout_impl(desc, dx_lora, p, seed, offset, counter, dx, dx_sum, stream);
+}
+
 dora_status dora_probe_copy(const void* src, void* dst, size_t bytes, void* stream)
 {
     DORA_REQ_PTR(src); DORA_REQ_PTR(dst);
@@ -1208,7 +1355,8 @@ const char* dora_trace_name(int kernel_id)
     static const char* names[DORA_K_COUNT] = {
         "norm_cross_WAt", "gram_AAt", "gram_reduce", "ba_sq_BGB", "norm_final", "mag_scale", "gemm_base_xWt",
         "gemm_h_xAt", "gemm_lora_hBt", "compose_fwd", "compose_bwd", "dm_final", "gemm_dh_dzB", "gemm_dx",
-        "gemm_dA", "gemm_dB", "probe_copy", "probe_mfma", "gemm_fused_fwd", "splitk_reduce"};
+        "gemm_dA", "gemm_dB", "probe_copy", "probe_mfma", "gemm_fused_fwd", "splitk_reduce",
+        "quantize", "dequantize", "dropout"};
     return (kernel_id >= 0 && kernel_id < DORA_K_COUNT) ? names[kernel_id] : "?";
 }
 

@@ -1,0 +1,61 @@
+// 4-bit frozen weights: what a word of codes stands for, and eight elements of a storage type at a time.
+#pragma once
+
+#include "common.hpp"
+
+namespace dora {
+namespace {
+
+// Eight consecutive elements of a row, aligned to 16 bytes.
+template <typename T> struct Eight;
+template <int DT>
+struct Eight16 {
+    typedef Elem16<DT> E;
+    static __device__ __forceinline__ void load(const void* p, float (&f)[8])
+    {
+        const uint4 r = *reinterpret_cast<const uint4*>(p);
+        f[0] = E::lo(r.x); f[1] = E::hi(r.x); f[2] = E::lo(r.y); f[3] = E::hi(r.y);
+        f[4] = E::lo(r.z); f[5] = E::hi(r.z); f[6] = E::lo(r.w); f[7] = E::hi(r.w);
+    }
+    static __device__ __forceinline__ void store(void* p, const float (&f)[8])
+    {
+        uint4 r;
+        r.x = E::pack2(f[0], f[1]); r.y = E::pack2(f[2], f[3]); r.z = E::pack2(f[4], f[5]); r.w = E::pack2(f[6], f[7]);
+        *reinterpret_cast<uint4*>(p) = r;
+    }
+    static __device__ __forceinline__ float one(const void* p, int64_t i) { return E::lo(static_cast<const uint16_t*>(p)[i]); }
+    static __device__ __forceinline__ void put(void* p, int64_t i, float v) { static_cast<uint16_t*>(p)[i] = (uint16_t)E::pack2(v, 0.f); }
+};
+template <> struct Eight<bf16_t> : Eight16<DT_BF16> {};
+template <> struct Eight<f16_t> : Eight16<DT_F16> {};
+template <> struct Eight<float> {
+    static __device__ __forceinline__ void load(const void* p, float (&f)[8])
+    {
+        const float4 a = static_cast<const float4*>(p)[0], b = static_cast<const float4*>(p)[1];
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    static __device__ __forceinline__ void store(void* p, const float (&f)[8])
+    {
+        static_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+        static_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    static __device__ __forceinline__ float one(const void* p, int64_t i) { return static_cast<const float*>(p)[i]; }
+    static __device__ __forceinline__ void put(void* p, int64_t i, float v) { static_cast<float*>(p)[i] = v; }
+};
+
+// The values of the eight codes of a word (before zero point and scale), in the order of their columns.
+template <int CODE>
+__device__ __forceinline__ void decode8(uint32_t w, float (&f)[8])
+{
+    if constexpr (CODE == DORA_QUANT_FP4) {
+        const f32x2_hw_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+        const f32x2_hw_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+        f[0] = a[0]; f[1] = a[1]; f[2] = b[0]; f[3] = b[1]; f[4] = c[0]; f[5] = c[1]; f[6] = d[0]; f[7] = d[1];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (float)((w >> (4 * j)) & 15u);
+    }
+}
+
+}  // namespace
+}  // namespace dora
