@@ -47,7 +47,8 @@ enum {
     DORA_K_QUANTIZE = 20,    /* dora_quantize                                          */
     DORA_K_DEQUANTIZE = 21,  /* 4-bit weight to storage: dora_dequantize, tiled routes */
     DORA_K_DROPOUT = 22,     /* dora_dropout, dora_dropout_backward                    */
-    DORA_K_COUNT = 23
+    DORA_K_QUANT_TOKENS = 23, /* y of a few tokens over a 4-bit weight                 */
+    DORA_K_COUNT = 24
 };
 void dora_trace_enable(int on);
 void dora_trace_select(uint64_t kernel_mask); /* bit k set = bracket launches of kernel id k (default: all) */

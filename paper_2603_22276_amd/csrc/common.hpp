@@ -345,6 +345,21 @@ hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int co
                            hipStream_t st);
 hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st);
 
+// forward of a few tokens over such a weight (quant_tokens.hip), as launch_few_tokens_y
+struct QuantTokensArgs {
+    const bf16_t* x;          // [T, d_in]
+    int T;
+    QuantWeight w;
+    const float* h_part;      // [h_slices][T][r]
+    int h_slices, r;
+    const bf16_t* b;          // [d_out, r]
+    float s, eps;
+    const float *m, *c;       // [d_out]
+    const bf16_t* bias;       // [d_out] or nullptr
+    bf16_t *y, *inner, *h_out;   // [T, d_out]; [T, d_out] or nullptr; [T, r] or nullptr
+};
+hipError_t launch_quant_tokens(const QuantTokensArgs& a, int dt, hipStream_t st);
+
 // ---- dropout with a mask that is drawn where it is needed (dropout.hip) -----------------------------
 struct DropoutArgs {
     const void *v, *add;      // add may be nullptr

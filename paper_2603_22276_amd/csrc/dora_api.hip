@@ -519,6 +519,13 @@ inline bool few_tokens(const dora_desc* d, bool one_product)
     return one_product ? r <= 128 && d->d_in >= 2048 && d->d_in <= 4096 : r <= 256 && d->d_in <= 4096;
 }
 
+// Forward of a few tokens over a 4-bit weight: two launches that stream A and W (few_tokens.hip, quant_tokens.hip).  A slice of h
+// is one buffer of 32-bit offsets.
+inline bool quant_tokens(const dora_desc* d)
+{
+    return is16(d->dtype) && d->tokens > 0 && d->tokens <= 32 && d->tokens * d->r < (int64_t)1 << 29;
+}
+
 // scratch for the K slices of a [tokens, n] product over k whose N-side operand has rows of ldb
 inline size_t slice_floats(const dora_desc* d, int64_t n, int64_t k, int64_t ldb)
 {
@@ -527,7 +534,7 @@ inline size_t slice_floats(const dora_desc* d, int64_t n, int64_t k, int64_t ldb
 }
 
 void plan_fwd(const dora_desc* d, Bump& b, FwdPlan& p, bool need_norm, bool need_h, bool need_lora,
-              bool need_hs = false, bool need_base_a = false)
+              bool need_hs = false, bool need_base_a = false, bool quant = false)
 {
     memset(&p, 0, sizeof(p));
     if (need_norm) plan_norm(d, b, p.norm);
@@ -539,7 +546,7 @@ void plan_fwd(const dora_desc* d, Bump& b, FwdPlan& p, bool need_norm, bool need
     if (need_hs) p.hs = b.take_bytes((size_t)d->tokens * d->r * esize(d->dtype));
     if (need_base_a) p.base_a = b.take_bytes((size_t)d->tokens * d->d_out * esize(d->dtype));
     // (where the K-concatenated product gives way to few_tokens, the compose pass does too)
-    size_t slices = few_tokens(d, false) ? (size_t)few_tokens_h_slices(d->tokens, d->r, d->d_in) * d->tokens * d->r : 0;
+    size_t slices = few_tokens(d, false) || (quant && quant_tokens(d)) ? (size_t)few_tokens_h_slices(d->tokens, d->r, d->d_in) * d->tokens * d->r : 0;
     slices = std::max({slices, slice_floats(d, d->r, d->d_in, d->d_in), slice_floats(d, d->d_out, d->d_in, d->d_in)});
     if (slices) p.skp = b.take<float>(slices);
 }
@@ -635,6 +642,23 @@ dora_status forward_few_tokens(const dora_desc* d, const void* x, const void* W,
     return DORA_OK;
 }
 
+// the same over a 4-bit weight
+dora_status forward_quant_tokens(const dora_desc* d, const void* x, const QuantWeight& w, const void* A, const void* B, const float* m,
+                                 const float* c, const void* bias, void* y, void* saved_h, void* saved_inner, float* h_part, hipStream_t st)
+{
+    FewTokensArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = (const bf16_t*)x; a.T = (int)d->tokens; a.K = (int)d->d_in;
+    a.w = (const bf16_t*)A; a.N = (int)d->r;
+    a.ksplit = few_tokens_h_slices(d->tokens, d->r, d->d_in);
+    a.part = h_part;
+    DORA_HIP(launch_few_tokens_h(a, dt_of(d->dtype), st));
+    const QuantTokensArgs q{(const bf16_t*)x, (int)d->tokens, w, h_part, a.ksplit, (int)d->r, (const bf16_t*)B, d->s, eff_eps(d), m, c,
+                            (const bf16_t*)bias, (bf16_t*)y, (bf16_t*)saved_inner, (bf16_t*)saved_h};
+    DORA_HIP(launch_quant_tokens(q, dt_of(d->dtype), st));
+    return DORA_OK;
+}
+
 }  // namespace
 }  // namespace dora
 
@@ -675,7 +699,7 @@ size_t dora_workspace_bytes(const dora_desc* desc, int phase)
         case DORA_PHASE_FORWARD_DROPOUT: { FwdPlan p; plan_fwd(desc, b, p, true, true, true, true, true); break; }
         case DORA_PHASE_BACKWARD_DROPOUT: { BwdPlan p; plan_bwd(desc, b, p, true, true, true, true); break; }
         case DORA_PHASE_NORM_QUANT: { NormPlan n; take_weight(desc, b); plan_norm(desc, b, n); break; }
-        case DORA_PHASE_FORWARD_QUANT: { FwdPlan p; take_weight(desc, b); plan_fwd(desc, b, p, true, true, true, true, true); break; }
+        case DORA_PHASE_FORWARD_QUANT: { FwdPlan p; take_weight(desc, b); plan_fwd(desc, b, p, true, true, true, true, true, true); break; }
         case DORA_PHASE_BACKWARD_QUANT: { BwdPlan p; take_weight(desc, b); plan_bwd(desc, b, p, true, true, true, true); break; }
         default: return 0;
     }
@@ -858,12 +882,14 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     const bool dropout = (x_lora != nullptr);
     const bool f32_plain = desc->dtype == DORA_F32 && !dropout;
     const bool need_lora = !one_product && !f32_plain && saved_inner == nullptr;
-    const bool need_weight = wq && (need_norm || desc->tokens > 0);
+    // over 4 bits the streaming launch is the faster one wherever it runs; it takes the weight as it is
+    const bool streamed = !dropout && (wq ? quant_tokens(desc) : few_tokens(desc, one_product));
+    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && !streamed));
     if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     FwdPlan p;
     if (need_weight) take_weight(desc, sizing);
-    plan_fwd(desc, sizing, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout);
+    plan_fwd(desc, sizing, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout, wq != nullptr);
     if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
     Bump b(ws);
     hipStream_t s = (hipStream_t)stream;
@@ -872,14 +898,13 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
         DORA_HIP(launch_dequantize(desc->dtype, *wq, read_back, s));
         W = read_back;
     }
-    plan_fwd(desc, b, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout);
+    plan_fwd(desc, b, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout, wq != nullptr);
     const int T = (int)desc->tokens, d_out = (int)desc->d_out, d_in = (int)desc->d_in, r = (int)desc->r;
 
     float* const gm1 = one_product ? nullptr : p.gm1;   // only the compose pass reads g - 1
     MagOut mag{m, eff_eps(desc), p.g, gm1, false};
     const float* c = w_norm;
     Waiting waiting;          // Eq. 5 and 6: g is read by the last launch of the tiled routes only
-    const bool streamed = !dropout && few_tokens(desc, one_product);
     if (need_norm) {
         float* cw = w_norm_out ? w_norm_out : p.c;
         if ((st = norm_impl(desc, W, A, B, cw, p.norm, s, nullptr, nullptr, nullptr, &mag, T > 0 && !streamed ? &waiting : nullptr)) != DORA_OK)
@@ -890,7 +915,8 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     }
     if (T == 0) return DORA_OK;
     if (streamed)
-        return forward_few_tokens(desc, x, W, A, B, m, c, bias, y, saved_h, saved_inner, p.skp, s);
+        return wq ? forward_quant_tokens(desc, x, *wq, A, B, m, c, bias, y, saved_h, saved_inner, p.skp, s)
+                  : forward_few_tokens(desc, x, W, A, B, m, c, bias, y, saved_h, saved_inner, p.skp, s);
     if (!mag.done) DORA_HIP(launch_mag_scale(m, c, eff_eps(desc), p.g, gm1, d_out, s));
     void* h = saved_h ? saved_h : p.h;
     if (one_product) {
@@ -1356,7 +1382,7 @@ const char* dora_trace_name(int kernel_id)
         "norm_cross_WAt", "gram_AAt", "gram_reduce", "ba_sq_BGB", "norm_final", "mag_scale", "gemm_base_xWt",
         "gemm_h_xAt", "gemm_lora_hBt", "compose_fwd", "compose_bwd", "dm_final", "gemm_dh_dzB", "gemm_dx",
         "gemm_dA", "gemm_dB", "probe_copy", "probe_mfma", "gemm_fused_fwd", "splitk_reduce",
-        "quantize", "dequantize", "dropout"};
+        "quantize", "dequantize", "dropout", "quant_tokens"};
     return (kernel_id >= 0 && kernel_id < DORA_K_COUNT) ? names[kernel_id] : "?";
 }
 

@@ -57,5 +57,43 @@ __device__ __forceinline__ void decode8(uint32_t w, float (&f)[8])
     }
 }
 
+// The same as one MFMA fragment: eight 16-bit numbers, exact (the codes of DORA_QUANT_INT4 as 0 .. 15).  A nibble q is the E4M3
+// float q 2^-9 (its lowest sixteen codes run linearly through the subnormals), so the converter of that type, with a scale of
+// 512, makes two integers of two bytes; nibbles are sorted into column order on the way.
+template <int CODE, int DT>
+__device__ __forceinline__ bf16x8_t decode_fragment(uint32_t w)
+{
+    typedef uint32_t u32x4_frag_t __attribute__((ext_vector_type(4)));
+    u32x4_frag_t v;
+    if constexpr (CODE == DORA_QUANT_FP4) {
+        if constexpr (DT == DT_BF16) {
+            v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0));
+            v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1));
+            v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2));
+            v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3));
+        } else {
+            v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0));
+            v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1));
+            v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 2));
+            v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 3));
+        }
+    } else {
+        const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+        const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x05010400u), b = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+        if constexpr (DT == DT_BF16) {
+            v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 512.f, false));
+            v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 512.f, true));
+            v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.f, false));
+            v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.f, true));
+        } else {
+            v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 512.f, false));
+            v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 512.f, true));
+            v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 512.f, false));
+            v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 512.f, true));
+        }
+    }
+    return __builtin_bit_cast(bf16x8_t, v);
+}
+
 }  // namespace
 }  // namespace dora
