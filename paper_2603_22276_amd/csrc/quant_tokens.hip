@@ -404,15 +404,23 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
     }
 }
 
+// Rows of a workgroup and ring slots: us of a forward, one after the other over as many sets of weights and inputs as make 600 MB.
+//  - 16 rows make 256 workgroups of 4096 rows of W.  Beyond, they would read x once more for every round, so 32 of them up to
+//    8192 rows and 64 past that: 8192 x 8192, r 64, 32 tokens 31.5, 22.7 and 26.9 us with 16, 32 and 64 rows, 16 tokens 24.4, 20.4,
+//    25.2; 14336 x 4096, 27 tokens 35.6, 24.9, 21.3.  Up to four tokens x hardly counts, and 16 rows do up to 8192 (8192 x 8192, 1
+//    token 16.1, 16.1 and 18.6 us; 14336 x 4096 20.3, 18.7, 15.4).
+//  - One ring slot to each of eight waves: more LDS leaves room for one workgroup on a CU, and the other's prologue no longer stands
+//    beside this one's products (27648 x 5120, 16 tokens 36.3 us with three slots to each of four waves, 33.5 this way; 1 token 30.1
+//    with two slots to each of eight, 28.2).  Two slots where they are small enough (4096 x 4096, r 384, 1 token 11.8 and 11.1).
 template <int CODE, int SUB, int DT>
 hipError_t launch_shape(const QuantTokensArgs& a, hipStream_t st)
 {
-#define DORA_QUANT_TOKENS(TB, XR, MR, NW, D) \
-    quant_tokens_kernel<TB, XR, MR, NW, D, CODE, SUB, DT><<<dim3((unsigned)((a.w.d_out + MR * 16 - 1) / (MR * 16))), dim3(64 * NW), 0, st>>>(a)
-    const bool wide = a.w.d_out > 8192;
-    if (a.T <= 4) { if (wide) DORA_QUANT_TOKENS(1, 4, 4, 8, 2); else DORA_QUANT_TOKENS(1, 4, 1, 8, 4); }
-    else if (a.T <= 16) { if (wide) DORA_QUANT_TOKENS(1, 16, 4, 4, 3); else DORA_QUANT_TOKENS(1, 16, 1, 8, 2); }
-    else { if (wide) DORA_QUANT_TOKENS(2, 32, 4, 4, 2); else DORA_QUANT_TOKENS(2, 32, 1, 4, 3); }
+#define DORA_QUANT_TOKENS(TB, XR, MR, D) \
+    quant_tokens_kernel<TB, XR, MR, 8, D, CODE, SUB, DT><<<dim3((unsigned)((a.w.d_out + MR * 16 - 1) / (MR * 16))), dim3(512), 0, st>>>(a)
+    const bool narrow = a.w.d_out <= 4096, wide = a.w.d_out > 8192;
+    if (a.T <= 4) { if (wide) DORA_QUANT_TOKENS(1, 4, 4, 1); else DORA_QUANT_TOKENS(1, 4, 1, 2); }
+    else if (a.T <= 16) { if (wide) DORA_QUANT_TOKENS(1, 16, 4, 1); else if (narrow) DORA_QUANT_TOKENS(1, 16, 1, 1); else DORA_QUANT_TOKENS(1, 16, 2, 1); }
+    else { if (wide) DORA_QUANT_TOKENS(2, 32, 4, 1); else if (narrow) DORA_QUANT_TOKENS(2, 32, 1, 1); else DORA_QUANT_TOKENS(2, 32, 2, 1); }
 #undef DORA_QUANT_TOKENS
     return hipGetLastError();
 }

@@ -32,7 +32,7 @@ def split_at_branches(body):
 
 
 @pytest.mark.skipif(not os.path.exists(T.HIPCC), reason="hipcc not available")
-@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 72)])
+@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 96)])
 def test_no_register_is_used_before_its_read_has_landed(tmp_path, monkeypatch, source, pattern, count):
     monkeypatch.setattr(T, "_transfer", N._transfer)
     kernels = kernels_of(tmp_path, source, pattern)
