@@ -48,7 +48,8 @@ enum {
     DORA_K_DEQUANTIZE = 21,  /* 4-bit weight to storage: dora_dequantize, tiled routes */
     DORA_K_DROPOUT = 22,     /* dora_dropout, dora_dropout_backward                    */
     DORA_K_QUANT_TOKENS = 23, /* y of a few tokens over a 4-bit weight                 */
-    DORA_K_COUNT = 24
+    DORA_K_QUANT_TILE = 24,  /* [x | h] [W | B]^T of more tokens over a 4-bit weight   */
+    DORA_K_COUNT = 25
 };
 void dora_trace_enable(int on);
 void dora_trace_select(uint64_t kernel_mask); /* bit k set = bracket launches of kernel id k (default: all) */

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(HERE, "libdora.so")
 DORA_F32, DORA_BF16, DORA_F16 = 0, 1, 2
 PHASE_NORM, PHASE_FORWARD, PHASE_BACKWARD, PHASE_BACKWARD_RECOMPUTE, PHASE_COMPOSE_BACKWARD, PHASE_FORWARD_DROPOUT, PHASE_BACKWARD_DROPOUT, PHASE_NORM_QUANT, PHASE_FORWARD_QUANT, PHASE_BACKWARD_QUANT = range(10)
 QUANT_INT4, QUANT_FP4 = 0, 1
-K_COUNT = 24
+K_COUNT = 25
 
 EXPORTS = (
     "dora_workspace_bytes", "dora_norm", "dora_norm_static", "dora_norm_static_max_bytes", "dora_base_sq", "dora_norm_cached", "dora_norm_terms", "dora_norm_assemble", "dora_mag_scale", "dora_compose", "dora_compose_backward",

@@ -360,6 +360,28 @@ struct QuantTokensArgs {
 };
 hipError_t launch_quant_tokens(const QuantTokensArgs& a, int dt, hipStream_t st);
 
+// forward of more tokens over such a weight (quant_tile.hip): h is there; part != nullptr: the sums of each slice of the columns
+// instead of y and inner
+struct QuantTileArgs {
+    const bf16_t* x;          // [T, d_in]
+    int T;
+    QuantWeight w;
+    const bf16_t* h;          // [T, r]
+    int r;
+    const bf16_t* b;          // [d_out, r]
+    float s, eps;
+    const float *m, *c;       // [d_out]
+    const bf16_t* bias;       // [d_out] or nullptr
+    bf16_t *y, *inner;        // [T, d_out]; inner may be nullptr
+    int ksplit;
+    float *part, *g;          // [ksplit][T][d_out]; with it [d_out]: receives g
+    int token_tiles, row_tiles;   // (set by the launch)
+};
+// scales come eight groups at a time, from words of memory
+inline bool quant_tile_takes(const QuantWeight& w) { return w.groups >= 8 && w.groups % 2 == 0; }
+int quant_tile_slices(int64_t tokens, const QuantWeight& w);
+hipError_t launch_quant_tile(QuantTileArgs a, int dt, hipStream_t st);
+
 // ---- dropout with a mask that is drawn where it is needed (dropout.hip) -----------------------------
 struct DropoutArgs {
     const void *v, *add;      // add may be nullptr

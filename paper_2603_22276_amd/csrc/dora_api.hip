@@ -526,6 +526,12 @@ inline bool quant_tokens(const dora_desc* d)
     return is16(d->dtype) && d->tokens > 0 && d->tokens <= 32 && d->tokens * d->r < (int64_t)1 << 29;
 }
 
+// and of more tokens, as long as decoding in the product costs less than reading the weight back (us, read back / decoded, weights
+// from memory: 33 tokens 1024 x 4096, r 64 32 / 26, 64 tokens 14336 x 4096 89 / 49, 256 tokens 4096 x 4096 48 / 46, 8192 x 8192 91 /
+// 76, 27648 x 5120 210 / 111; 384 tokens 53 / 53 and 103 / 106 at the first two of these, 1024 tokens 63 / 78).
+constexpr int64_t QUANT_TILE_MAX = 320;
+inline bool quant_tile(const dora_desc* d) { return is16(d->dtype) && d->tokens > 32 && d->tokens <= QUANT_TILE_MAX; }
+
 // scratch for the K slices of a [tokens, n] product over k whose N-side operand has rows of ldb
 inline size_t slice_floats(const dora_desc* d, int64_t n, int64_t k, int64_t ldb)
 {
@@ -548,6 +554,15 @@ void plan_fwd(const dora_desc* d, Bump& b, FwdPlan& p, bool need_norm, bool need
     // (where the K-concatenated product gives way to few_tokens, the compose pass does too)
     size_t slices = few_tokens(d, false) || (quant && quant_tokens(d)) ? (size_t)few_tokens_h_slices(d->tokens, d->r, d->d_in) * d->tokens * d->r : 0;
     slices = std::max({slices, slice_floats(d, d->r, d->d_in, d->d_in), slice_floats(d, d->d_out, d->d_in, d->d_in)});
+    if (quant && quant_tile(d)) {
+        // (whatever the groups)
+        QuantWeight w{};
+        w.d_out = (int)d->d_out; w.d_in = (int)d->d_in;
+        for (w.group_shift = 5; w.group_shift <= 6; ++w.group_shift) {
+            const int ks = quant_tile_slices(d->tokens, w);
+            if (ks > 1) slices = std::max(slices, (size_t)ks * d->tokens * d->d_out);
+        }
+    }
     if (slices) p.skp = b.take<float>(slices);
 }
 
@@ -884,7 +899,8 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     const bool need_lora = !one_product && !f32_plain && saved_inner == nullptr;
     // over 4 bits the streaming launch is the faster one wherever it runs; it takes the weight as it is
     const bool streamed = !dropout && (wq ? quant_tokens(desc) : few_tokens(desc, one_product));
-    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && !streamed));
+    const bool tiled = wq && !dropout && quant_tile(desc) && quant_tile_takes(*wq);
+    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && !streamed && !tiled));
     if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     FwdPlan p;
@@ -917,8 +933,20 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     if (streamed)
         return wq ? forward_quant_tokens(desc, x, *wq, A, B, m, c, bias, y, saved_h, saved_inner, p.skp, s)
                   : forward_few_tokens(desc, x, W, A, B, m, c, bias, y, saved_h, saved_inner, p.skp, s);
-    if (!mag.done) DORA_HIP(launch_mag_scale(m, c, eff_eps(desc), p.g, gm1, d_out, s));
     void* h = saved_h ? saved_h : p.h;
+    if (tiled) {
+        Seg s1{x, d_in, A, d_in, d_in};
+        DORA_HIP(contract(desc->dtype, true, true, T, r, &s1, 1, 1.f, h, r, false, DORA_K_GEMM_H, s, p.skp, nullptr, 0.f, &waiting));
+        DORA_HIP(launch_waiting(waiting, s));
+        const int ks = quant_tile_slices(T, *wq);
+        const QuantTileArgs q{(const bf16_t*)x, T, *wq, (const bf16_t*)h, r, (const bf16_t*)B, desc->s, eff_eps(desc), m, c, (const bf16_t*)bias,
+                              (bf16_t*)y, (bf16_t*)saved_inner, ks, ks > 1 ? p.skp : nullptr, p.g, 0, 0};
+        DORA_HIP(launch_quant_tile(q, dt_of(desc->dtype), s));
+        if (ks == 1) return DORA_OK;
+        DORA_HIP(launch_splitk_reduce(p.skp, ks, (int64_t)T * d_out, desc->dtype, y, 1.f, saved_inner, s, p.g, bias, d_out));
+        return DORA_OK;
+    }
+    if (!mag.done) DORA_HIP(launch_mag_scale(m, c, eff_eps(desc), p.g, gm1, d_out, s));
     if (one_product) {
         // h = x A^T, written twice from the same accumulators: as it is (the saved tensor) and scaled by s
         Seg s1{x, d_in, A, d_in, d_in};
@@ -1382,7 +1410,7 @@ const char* dora_trace_name(int kernel_id)
         "norm_cross_WAt", "gram_AAt", "gram_reduce", "ba_sq_BGB", "norm_final", "mag_scale", "gemm_base_xWt",
         "gemm_h_xAt", "gemm_lora_hBt", "compose_fwd", "compose_bwd", "dm_final", "gemm_dh_dzB", "gemm_dx",
         "gemm_dA", "gemm_dB", "probe_copy", "probe_mfma", "gemm_fused_fwd", "splitk_reduce",
-        "quantize", "dequantize", "dropout", "quant_tokens"};
+        "quantize", "dequantize", "dropout", "quant_tokens", "quant_tile"};
     return (kernel_id >= 0 && kernel_id < DORA_K_COUNT) ? names[kernel_id] : "?";
 }
 

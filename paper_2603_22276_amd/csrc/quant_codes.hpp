@@ -1,7 +1,7 @@
 // 4-bit frozen weights: what a word of codes stands for, and eight elements of a storage type at a time.
 #pragma once
 
-#include "common.hpp"
+#include "lds_tile.hpp"
 
 namespace dora {
 namespace {
@@ -95,5 +95,48 @@ __device__ __forceinline__ bf16x8_t decode_fragment(uint32_t w)
     return __builtin_bit_cast(bf16x8_t, v);
 }
 
+// ---- what the kernels that multiply with codes share ------------------------------------------------
+constexpr uint32_t OUTSIDE = 0xFFFFFFFFu;              // beyond every descriptor: loads zeros
+constexpr int BLOCK_K = 128;                           // columns of a step of the kernels that multiply with codes
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const char* lds_cptr_t;
+
+template <int OFF>
+__device__ __forceinline__ uint64_t lds_read_b64(uint32_t addr)
+{
+    static_assert(OFF >= 0 && OFF < 65536, "ds_read offset field is 16 bits");
+    uint64_t v;
+    asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr)
+{
+    static_assert(OFF >= 0 && OFF < 65536, "ds_read offset field is 16 bits");
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read_u16(uint32_t addr)
+{
+    static_assert(OFF >= 0 && OFF < 65536, "ds_read offset field is 16 bits");
+    uint32_t v;
+    asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+// (the writes too: the compiler would have them wait for the loads to the LDS that are in flight)
+__device__ __forceinline__ void lds_write_b128(uint32_t addr, const uint4& v)
+{
+    asm volatile("ds_write_b128 %0, %1" ::"v"(addr), "v"(__builtin_bit_cast(bf16x8_t, v)) : "memory");
+}
+__device__ __forceinline__ void lds_write_b32(uint32_t addr, uint32_t v) { asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory"); }
+
+// 16 bytes per lane from memory into 1 KB of LDS
+__device__ __forceinline__ void load_1k(char* lds, __amdgpu_buffer_rsrc_t rs, uint32_t off, uint32_t soffset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr_t)lds, 16, off, soffset, 0, 0);
+}
 }  // namespace
 }  // namespace dora

@@ -11,44 +11,11 @@
 // Codes and x straight from memory in the MFMA's own layout, without the LDS: sixteen lanes in a row then are sixteen rows, each
 // a line of its own to the L1 (14336 x 4096, r 8, 27 tokens, codes from memory 25 us, 20 this way).  Scales and zero points one at
 // a time from memory cost the same way; they come through the LDS, a piece of the columns at a time.
-#include "lds_tile.hpp"
 #include "quant_codes.hpp"
 
 namespace dora {
 namespace {
 
-constexpr uint32_t OUTSIDE = 0xFFFFFFFFu;              // beyond every descriptor: loads zeros
-constexpr int BLOCK_K = 128;
-
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) const char* lds_cptr_t;
-
-template <int OFF>
-__device__ __forceinline__ uint64_t lds_read_b64(uint32_t addr)
-{
-    static_assert(OFF >= 0 && OFF < 65536, "ds_read offset field is 16 bits");
-    uint64_t v;
-    asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
-}
-__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ds_read_b32 %0, %1" : "=v"(v) : "v"(addr));
-    return v;
-}
-// (the writes too: the compiler would have them wait for the loads to the LDS that are in flight)
-__device__ __forceinline__ void lds_write_b128(uint32_t addr, const uint4& v)
-{
-    asm volatile("ds_write_b128 %0, %1" ::"v"(addr), "v"(__builtin_bit_cast(bf16x8_t, v)) : "memory");
-}
-__device__ __forceinline__ void lds_write_b32(uint32_t addr, uint32_t v) { asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory"); }
-
-// 16 bytes per lane from memory into 1 KB of LDS
-__device__ __forceinline__ void load_1k(char* lds, __amdgpu_buffer_rsrc_t rs, uint32_t off, uint32_t soffset)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr_t)lds, 16, off, soffset, 0, 0);
-}
 // all LDS reads so far, these fragments among them
 template <int TB>
 __device__ __forceinline__ void landed(bf16x8_t (&f)[TB])
@@ -283,13 +250,13 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
                 }
             } else {
 #pragma unroll
-                for (int n = 0; n < 4; ++n) w[i][n] = lds_read_b32(slot_lds + rw_at[n] + i * 1024);
+                for (int n = 0; n < 4; ++n) w[i][n] = lds_read_b32<i * 1024>(slot_lds + rw_at[n]);
             }
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
                 int g = (b * BLOCK_K + n * SUB * 32) >> p.w.group_shift;
                 g = (g < p.w.groups ? g : p.w.groups - 1) - g_first;   // (past the end: times a sum of zeros)
-                sz[i][n] = lds_read_b32(scales_lds + (uint32_t)((i * 16 + l16) * SCALES_LD + g) * 4u);
+                sz[i][n] = lds_read_b32<i * 64 * SCALES_LD>(scales_lds + (uint32_t)(l16 * SCALES_LD + g) * 4u);
             }
         });
         wait_lgkmcnt<0>();

@@ -32,9 +32,11 @@ def split_at_branches(body):
 
 
 @pytest.mark.skipif(not os.path.exists(T.HIPCC), reason="hipcc not available")
-@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 96)])
+@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 96),
+                                                  ("quant_tile.hip", "quant_tile_kernel", 30)])
 def test_no_register_is_used_before_its_read_has_landed(tmp_path, monkeypatch, source, pattern, count):
-    monkeypatch.setattr(T, "_transfer", N._transfer)
+    # (a spill of a register whose value is on its way would be the same fault)
+    monkeypatch.setattr(T, "_transfer", lambda state, ins, *a: N._transfer(state, ["global_" + t if t.startswith("scratch_") else t for t in ins], *a))
     kernels = kernels_of(tmp_path, source, pattern)
     assert len(kernels) == count
     for name, body in kernels.items():
