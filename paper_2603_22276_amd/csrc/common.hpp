@@ -343,7 +343,13 @@ struct QuantWeight {          // a dora_quant and its shape
 inline int quant_groups(int d_in, int group_shift) { return (int)(((int64_t)d_in + ((int64_t)1 << group_shift) - 1) >> group_shift); }
 hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int code, int group_shift, void* q, void* scale, void* zero,
                            hipStream_t st);
-hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st);
+struct MagScaleArgs {         // g = m / max(c, eps), gm1 = g - 1 (either may be nullptr)
+    const float *m, *c;
+    float eps;
+    float *g, *gm1;
+};
+// mag.m != nullptr: Eq. 6 in the same launch
+hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st, const MagScaleArgs& mag = MagScaleArgs{});
 
 // forward of a few tokens over such a weight (quant_tokens.hip), as launch_few_tokens_y
 struct QuantTokensArgs {

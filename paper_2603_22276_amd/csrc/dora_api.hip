@@ -909,16 +909,18 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
     Bump b(ws);
     hipStream_t s = (hipStream_t)stream;
-    if (need_weight) {
-        void* const read_back = take_weight(desc, b);
-        DORA_HIP(launch_dequantize(desc->dtype, *wq, read_back, s));
-        W = read_back;
-    }
+    void* const read_back = need_weight ? take_weight(desc, b) : nullptr;
     plan_fwd(desc, b, p, need_norm, saved_h == nullptr, need_lora, one_product, dropout, wq != nullptr);
     const int T = (int)desc->tokens, d_out = (int)desc->d_out, d_in = (int)desc->d_in, r = (int)desc->r;
 
     float* const gm1 = one_product ? nullptr : p.gm1;   // only the compose pass reads g - 1
     MagOut mag{m, eff_eps(desc), p.g, gm1, false};
+    if (need_weight) {
+        const bool with_g = !need_norm && !streamed && !tiled;   // the norm is there: g is formed beside the weight
+        DORA_HIP(launch_dequantize(desc->dtype, *wq, read_back, s, with_g ? MagScaleArgs{m, w_norm, mag.eps, p.g, gm1} : MagScaleArgs{}));
+        mag.done = with_g;
+        W = read_back;
+    }
     const float* c = w_norm;
     Waiting waiting;          // Eq. 5 and 6: g is read by the last launch of the tiled routes only
     if (need_norm) {

@@ -47,8 +47,9 @@ __device__ __forceinline__ uint32_t lanes_pair_max(uint32_t v, int lanes)
 // A group belongs to `lanes` = min(64, group / 8) lanes of a wave, eight weights to a lane at a time; the extremes of the group
 // meet by lane exchanges, so a weight is read once (groups above 512: twice, the second time from the L2).  16-bit floats are
 // ordered as their bits are: the extremes are found two at a time, the largest positive as it is and the most negative as the largest
-// number with the sign bit (both of them wholes, and exponents of ones show infinities and NaN).  Bound: memory, and the vector
-// instructions of rounding beside it: 14336 x 4104 in fp16 with zero points, groups of 64, THIS us, RATE TB/s.
+// number with the sign bit; exponents of ones show infinities and NaN.  Bound: memory, and the vector instructions of rounding
+// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us,
+// 3.5 TB/s (65 with the extremes, the eight quotients and the eight codes of a thread one by one).
 //
 // Scales have four significant bits.  A symmetric code (at most 3 bits of odd part, 4 with a zero point) times such a scale
 // has 8 at most, so the weight that codes and scale stand for is a bf16 and an fp16 number without rounding, and every path
@@ -152,12 +153,22 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
     }
 }
 
-// Eight weights to a thread, four times: 4 bytes of codes in, 16 (32) out.
+// Eight weights to a thread, four times: 4 bytes of codes in, 16 (32) out.  Bound: memory (14336 x 4104, groups of 64, fp16: 24 us, 6.2
+// TB/s).  The workgroups past those form Eq. 6 for the caller, a launch of its own otherwise (4.7 us of 14336 rows).
 template <typename T, int CODE, bool ZERO>
-__global__ __launch_bounds__(256) void dequantize_kernel(QuantWeight w, T* out, uint32_t words, uint32_t per_row)
+__global__ __launch_bounds__(256) void dequantize_kernel(QuantWeight w, T* out, uint32_t words, uint32_t per_row, MagScaleArgs mag)
 {
     typedef Eight<T> V;
     constexpr int U = 4;
+    const uint32_t own = (words + 256u * U - 1) / (256u * U);
+    if (blockIdx.x >= own) {
+        const int64_t j = (int64_t)(blockIdx.x - own) * 256 + threadIdx.x;
+        if (j >= w.d_out) return;
+        const float c = mag.c[j], cc = (c < mag.eps) ? mag.eps : c, m = mag.m[j];
+        if (mag.g) mag.g[j] = m / cc;
+        if (mag.gm1) mag.gm1[j] = (m - cc) / cc;
+        return;
+    }
     const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
     uint32_t q[U];
     float s[U], z[U];
@@ -195,14 +206,14 @@ hipError_t quantize_t(const QuantizeArgs& a, int code, hipStream_t st)
 }
 
 template <typename T>
-hipError_t dequantize_t(const QuantWeight& w, void* out, hipStream_t st)
+hipError_t dequantize_t(const QuantWeight& w, void* out, const MagScaleArgs& mag, hipStream_t st)
 {
     const uint32_t per_row = (uint32_t)w.d_in / 8, words = (uint32_t)w.d_out * per_row;   // (d_out d_in < 2^31)
-    const dim3 grid((words + 1023) / 1024), block(256);
+    const dim3 grid((words + 1023) / 1024 + (mag.m ? (unsigned)(w.d_out + 255) / 256 : 0)), block(256);
     T* const o = static_cast<T*>(out);
-    if (w.code == DORA_QUANT_FP4) dequantize_kernel<T, DORA_QUANT_FP4, false><<<grid, block, 0, st>>>(w, o, words, per_row);
-    else if (w.zero) dequantize_kernel<T, DORA_QUANT_INT4, true><<<grid, block, 0, st>>>(w, o, words, per_row);
-    else dequantize_kernel<T, DORA_QUANT_INT4, false><<<grid, block, 0, st>>>(w, o, words, per_row);
+    if (w.code == DORA_QUANT_FP4) dequantize_kernel<T, DORA_QUANT_FP4, false><<<grid, block, 0, st>>>(w, o, words, per_row, mag);
+    else if (w.zero) dequantize_kernel<T, DORA_QUANT_INT4, true><<<grid, block, 0, st>>>(w, o, words, per_row, mag);
+    else dequantize_kernel<T, DORA_QUANT_INT4, false><<<grid, block, 0, st>>>(w, o, words, per_row, mag);
     return hipGetLastError();
 }
 
@@ -217,11 +228,11 @@ hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int co
     return dtype == DORA_F16 ? quantize_t<f16_t>(a, code, st) : quantize_t<bf16_t>(a, code, st);
 }
 
-hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st)
+hipError_t launch_dequantize(int dtype, const QuantWeight& w, void* out, hipStream_t st, const MagScaleArgs& mag)
 {
     TraceScope ts(DORA_K_DEQUANTIZE, st);
-    if (dtype == DORA_F32) return dequantize_t<float>(w, out, st);
-    return dtype == DORA_F16 ? dequantize_t<f16_t>(w, out, st) : dequantize_t<bf16_t>(w, out, st);
+    if (dtype == DORA_F32) return dequantize_t<float>(w, out, mag, st);
+    return dtype == DORA_F16 ? dequantize_t<f16_t>(w, out, mag, st) : dequantize_t<bf16_t>(w, out, mag, st);
 }
 
 }  // namespace dora

@@ -4,8 +4,8 @@
 // A workgroup owns 16 MR rows of W; its waves take the blocks of 128 columns in turn, each with an LDS ring of its own for codes
 // and token rows (buffer_load ... lds, no barrier: only its own vmcnt).  Codes become 16-bit integers (or E2M1 floats) exactly,
 // products are summed in fp32 within a group, and the group's sum is multiplied by the scale in fp32: no weight is rounded,
-// whatever the scale.  A zero point enters as zero times the sum of x over the group, which one more MFMA against ones gives for
-// all rows.  Which columns a lane multiplies in a k-step is free as long as the x fragments take the same ones and a k-step stays
+// whatever the scale.  A zero point enters as the addend of the group's first MFMA, its negative times the sum of x over the group,
+// which one more MFMA against a constant gives for all rows (-8 times it where the zero point is the same everywhere).  Which columns a lane multiplies in a k-step is free as long as the x fragments take the same ones and a k-step stays
 // within a group: a lane's share of a group is consecutive, so it is one read of 16, 8 or 4 bytes of codes.
 //
 // Codes and x straight from memory in the MFMA's own layout, without the LDS: sixteen lanes in a row then are sixteen rows, each
@@ -37,7 +37,7 @@ struct Slot {
 
 // TB: blocks of 16 tokens; XR: token rows that are loaded (4, or all); MR: blocks of 16 rows of W; NW: waves; D: ring slots of a
 // wave; SUB: k-steps of 32 to a scale
-template <int TB, int XR, int MR, int NW, int D, int CODE, int SUB, int DT>
+template <int TB, int XR, int MR, int NW, int D, int CODE, int SUB, bool ZERO, int DT>
 __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p)
 {
     typedef Elem16<DT> E;
@@ -110,14 +110,13 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
             const int row = wave + i * NW;
             const int64_t at = (int64_t)(n0 + (row < rows ? row : rows - 1)) * p.w.groups + first + g;
             sc[i] = scale[at];
-            zc[i] = INT ? (zero ? zero : scale)[at] : 0u;
+            zc[i] = ZERO ? zero[at] : 0u;
         }
     };
     auto put_scales = [&](int count, int g0) {
 #pragma unroll
         for (int i = 0; i < SROWS; ++i) {
-            const uint32_t z = !INT || zero ? zc[i] : DT == DT_BF16 ? 0x4100u : 0x4800u;   // 8
-            if (g0 + lane < count) lds_write_b32(scales_lds + (uint32_t)((wave + i * NW) * SCALES_LD + g0 + lane) * 4u, sc[i] | z << 16);
+            if (g0 + lane < count) lds_write_b32(scales_lds + (uint32_t)((wave + i * NW) * SCALES_LD + g0 + lane) * 4u, sc[i] | zc[i] << 16);
         }
     };
     auto groups_of = [&](int b0, int& first) {
@@ -227,8 +226,8 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
         rx_at[q] = (uint32_t)(S::W_BYTES + row * 256 + S::x_chunk(row, n * (SUB * 4) + lq * SUB + u) * 16);
         if (u == 0) rw_at[n] = (uint32_t)(l16 * 64 + S::w_chunk(l16, SUB == 4 ? lq : SUB == 2 ? n * 2 + (lq >> 1) : n) * 16 + (SUB == 2 ? (lq & 1) * 8 : SUB == 1 ? lq * 4 : 0));
     }
-    const uint32_t one = DT == DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
-    const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, u32x4_t{one, one, one, one});
+    const uint32_t addend = INT && !ZERO ? (DT == DT_BF16 ? 0xc100c100u : 0xc800c800u) : (DT == DT_BF16 ? 0x3f803f80u : 0x3c003c00u);   // -8, 1
+    const bf16x8_t constant = __builtin_bit_cast(bf16x8_t, u32x4_t{addend, addend, addend, addend});
     // the block in `slot`: codes, x and scales out of the LDS, then (refill) the slot's next loads, then the products
     auto multiply = [&](int b, int g_first, uint32_t slot_lds, auto&& refill) {
         bf16x8_t x[4][TB];
@@ -265,31 +264,38 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            f32x4_t sum[TB];
-            if constexpr (INT) {
+            f32x4_t first[TB];                         // what the products are added to: -8 (or 1) times the sum of x
 #pragma unroll
-                for (int j = 0; j < TB; ++j) {
-                    sum[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < TB; ++j) {
+                first[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if constexpr (INT) {
 #pragma unroll
-                    for (int q = n * SUB; q < (n + 1) * SUB; ++q) sum[j] = E::mfma16(x[q][j], ones, sum[j]);
+                    for (int q = n * SUB; q < (n + 1) * SUB; ++q) first[j] = E::mfma16(x[q][j], constant, first[j]);
                 }
             }
 #pragma unroll
             for (int i = 0; i < MR; ++i) {
+                const float s = E::lo(sz[i][n]);
                 f32x4_t part[TB];
 #pragma unroll
-                for (int j = 0; j < TB; ++j) part[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int j = 0; j < TB; ++j) {
+                    part[j] = first[j];
+                    if constexpr (ZERO) {
+                        const float z = -E::hi(sz[i][n]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) part[j][e] *= z;
+                    }
+                }
 #pragma unroll
                 for (int q = n * SUB; q < (n + 1) * SUB; ++q) {
                     const bf16x8_t wf = decode_fragment<CODE, DT>(w[i][q]);
 #pragma unroll
                     for (int j = 0; j < TB; ++j) part[j] = E::mfma16(x[q][j], wf, part[j]);
                 }
-                const float s = E::lo(sz[i][n]), z = E::hi(sz[i][n]);
 #pragma unroll
                 for (int j = 0; j < TB; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s, INT ? fmaf(-z, sum[j][e], part[j][e]) : part[j][e], acc[i][j][e]);
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s, part[j][e], acc[i][j][e]);
             }
         }
     };
@@ -379,11 +385,11 @@ __global__ __launch_bounds__(64 * NW) void quant_tokens_kernel(QuantTokensArgs p
 //  - One ring slot to each of eight waves: more LDS leaves room for one workgroup on a CU, and the other's prologue no longer stands
 //    beside this one's products (27648 x 5120, 16 tokens 36.3 us with three slots to each of four waves, 33.5 this way; 1 token 30.1
 //    with two slots to each of eight, 28.2).  Two slots where they are small enough (4096 x 4096, r 384, 1 token 11.8 and 11.1).
-template <int CODE, int SUB, int DT>
+template <int CODE, int SUB, bool ZERO, int DT>
 hipError_t launch_shape(const QuantTokensArgs& a, hipStream_t st)
 {
 #define DORA_QUANT_TOKENS(TB, XR, MR, D) \
-    quant_tokens_kernel<TB, XR, MR, 8, D, CODE, SUB, DT><<<dim3((unsigned)((a.w.d_out + MR * 16 - 1) / (MR * 16))), dim3(512), 0, st>>>(a)
+    quant_tokens_kernel<TB, XR, MR, 8, D, CODE, SUB, ZERO, DT><<<dim3((unsigned)((a.w.d_out + MR * 16 - 1) / (MR * 16))), dim3(512), 0, st>>>(a)
     const bool narrow = a.w.d_out <= 4096, wide = a.w.d_out > 8192;
     if (a.T <= 4) { if (wide) DORA_QUANT_TOKENS(1, 4, 4, 1); else DORA_QUANT_TOKENS(1, 4, 1, 2); }
     else if (a.T <= 16) { if (wide) DORA_QUANT_TOKENS(1, 16, 4, 1); else if (narrow) DORA_QUANT_TOKENS(1, 16, 1, 1); else DORA_QUANT_TOKENS(1, 16, 2, 1); }
@@ -391,16 +397,17 @@ hipError_t launch_shape(const QuantTokensArgs& a, hipStream_t st)
 #undef DORA_QUANT_TOKENS
     return hipGetLastError();
 }
+template <int SUB, int DT>
+hipError_t launch_code(const QuantTokensArgs& a, hipStream_t st)
+{
+    if (a.w.code == DORA_QUANT_FP4) return launch_shape<DORA_QUANT_FP4, SUB, false, DT>(a, st);
+    return a.w.zero ? launch_shape<DORA_QUANT_INT4, SUB, true, DT>(a, st) : launch_shape<DORA_QUANT_INT4, SUB, false, DT>(a, st);
+}
 template <int DT>
 hipError_t launch(const QuantTokensArgs& a, hipStream_t st)
 {
-    const int sub = a.w.group_shift >= 7 ? 4 : a.w.group_shift == 6 ? 2 : 1;
-    if (a.w.code == DORA_QUANT_FP4) {
-        if (sub == 4) return launch_shape<DORA_QUANT_FP4, 4, DT>(a, st);
-        return sub == 2 ? launch_shape<DORA_QUANT_FP4, 2, DT>(a, st) : launch_shape<DORA_QUANT_FP4, 1, DT>(a, st);
-    }
-    if (sub == 4) return launch_shape<DORA_QUANT_INT4, 4, DT>(a, st);
-    return sub == 2 ? launch_shape<DORA_QUANT_INT4, 2, DT>(a, st) : launch_shape<DORA_QUANT_INT4, 1, DT>(a, st);
+    if (a.w.group_shift >= 7) return launch_code<4, DT>(a, st);
+    return a.w.group_shift == 6 ? launch_code<2, DT>(a, st) : launch_code<1, DT>(a, st);
 }
 
 }  // namespace

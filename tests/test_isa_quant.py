@@ -32,7 +32,7 @@ def split_at_branches(body):
 
 
 @pytest.mark.skipif(not os.path.exists(T.HIPCC), reason="hipcc not available")
-@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 96),
+@pytest.mark.parametrize("source,pattern,count", [("quant_tokens.hip", "quant_tokens_kernel", 144),
                                                   ("quant_tile.hip", "quant_tile_kernel", 30)])
 def test_no_register_is_used_before_its_read_has_landed(tmp_path, monkeypatch, source, pattern, count):
     # (a spill of a register whose value is on its way would be the same fault)
