@@ -301,9 +301,10 @@ dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W
  *   x_lora : the adapter's own input as in dora_forward_dropout / dora_backward_dropout, or NULL: the plain module (as in
  *            the forward x itself).  In dora_backward_quant with x_lora, x is not read and may be NULL, and dx_lora receives
  *            the gradient of the adapter's input; without it dx_lora is not written.
- * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  The routes that multiply tiles
- * read W back into the workspace in the storage type first (2 or 4 bytes a weight), rounded once, which scales of up to four
- * significant bits and zero points of 0 to 15 do not show.
+ * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  In 16 bits the norm (s != 0, r <= 384,
+ * d_in a multiple of 32) and the plain forward of up to 320 tokens take the codes as they are, the latter within limits of shape; everything
+ * else reads W back into the workspace in the storage type first (2 or 4 bytes a weight).  Either way a product sees each weight
+ * rounded at most once, which scales of up to four significant bits and zero points of 0 to 15 do not show.
  */
 dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const void* A, const void* B, float* w_norm, void* ws,
                             size_t ws_bytes, void* stream);

@@ -181,7 +181,16 @@ int few_tokens_h_slices(int64_t tokens, int64_t r, int64_t d_in);
 hipError_t launch_few_tokens_h(const FewTokensArgs& a, int dt, hipStream_t st);
 hipError_t launch_few_tokens_y(const FewTokensArgs& a, int dt, hipStream_t st);
 
-// ---- the three sums of the row norm (16-bit storage, norm_rows.hip) ------------------------------
+// ---- a 4-bit frozen weight: a dora_quant and its shape -----------------------------------------------
+struct QuantWeight {
+    const uint32_t* q;        // [d_out][d_in / 8]
+    const void *scale, *zero; // [d_out][groups]; zero may be nullptr
+    int code, group_shift, groups;
+    int d_out, d_in;
+};
+inline int quant_groups(int d_in, int group_shift) { return (int)(((int64_t)d_in + ((int64_t)1 << group_shift) - 1) >> group_shift); }
+
+// ---- the three sums of the row norm (16-bit storage, norm_rows_body.hpp) ------------------------------
 constexpr int64_t NORM_ROWS_MAX_RANK = 384;
 struct NormRowsArgs {
     const bf16_t* w;        // [d_out, d_in]
@@ -190,8 +199,10 @@ struct NormRowsArgs {
     int d_out, d_in, r;
     int slices, tiles_per_slice;   // slices of tiles_per_slice column tiles of 128 each; none of them empty
     float* part;            // [3][slices][d_out]: base_sq, cross, ba_sq
+    QuantWeight q;          // instead of w: d_in a multiple of 32
 };
 hipError_t launch_norm_rows(const NormRowsArgs& a, int dt, hipStream_t st);
+hipError_t launch_norm_quant(const NormRowsArgs& a, int dt, hipStream_t st);   // (norm_quant.hip)
 
 // ---- fp32 products (sgemm_f32.hip) ----------------------------------------------------------------
 // C[M,N] = alpha * rowscale[m] * sum over segments of  ascale[k] Aop[m,k] * Bop[n,k], operands K-contiguous or K-strided as in
@@ -334,13 +345,6 @@ hipError_t launch_splitk_reduce(const float* partials, int ksplit, int64_t n, in
                                 Waiting* waiting = nullptr);
 
 // ---- 4-bit frozen weights (quant.hip) --------------------------------------------------------------
-struct QuantWeight {          // a dora_quant and its shape
-    const uint32_t* q;        // [d_out][d_in / 8]
-    const void *scale, *zero; // [d_out][groups]; zero may be nullptr
-    int code, group_shift, groups;
-    int d_out, d_in;
-};
-inline int quant_groups(int d_in, int group_shift) { return (int)(((int64_t)d_in + ((int64_t)1 << group_shift) - 1) >> group_shift); }
 hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int code, int group_shift, void* q, void* scale, void* zero,
                            hipStream_t st);
 struct MagScaleArgs {         // g = m / max(c, eps), gm1 = g - 1 (either may be nullptr)

@@ -225,7 +225,7 @@ void norm_split(int64_t d_out, int64_t d_in, int64_t r, int& ks_u, int& ks_g)
     ks_g = (int)best_g;
 }
 
-// Slices of the columns for the launch that forms the three sums (norm_rows.hip): the cheapest in rounds of workgroups, two
+// Slices of the columns for the launch that forms the three sums (norm_rows_body.hpp): the cheapest in rounds of workgroups, two
 // to a CU up to r 128, one beyond, counted in cycles of a tile (its share of reading W, or its MFMAs) and of what comes before
 // the first.
 void norm_slices(int64_t d_out, int64_t d_in, int64_t r, size_t fixed_bytes, size_t most_bytes, int& slices, int& tiles_per_slice)
@@ -392,13 +392,16 @@ hipError_t contract(int dtype, bool a_kc, bool b_kc, int M, int N, const Seg* se
 // G_out != nullptr: [r, r] fp32 receives the Gram matrix of Eq. 4.
 // waiting != nullptr: the last launch may be left there.
 // G is an operand of the B G product (16-bit): a rank whose Gram matrix cannot be one
+// The norm of a 4-bit weight whose sums come from the codes (norm_quant.hip): rows of codes in 16-byte pieces.  Elsewhere the norm
+// needs the weight read back.
+inline bool norm_of_codes(const dora_desc* d) { return is16(d->dtype) && d->s != 0.f && d->r <= NORM_ROWS_MAX_RANK && d->d_in % 32 == 0; }
 inline bool norm_refused(const dora_desc* d) { return is16(d->dtype) && d->s != 0.f && d->r * d->r >= MAX_ELEMS; }
 // Eq. 6 riding on the norm's last launch: set `done` when g / gm1 were written there
 struct MagOut { const float* m; float eps; float* g; float* gm1; bool done; };
 
 dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const void* B, float* c, const NormPlan& n,
                       hipStream_t st, const float* base_sq = nullptr, float* terms = nullptr, float* G_out = nullptr,
-                      MagOut* mag = nullptr, Waiting* waiting = nullptr)
+                      MagOut* mag = nullptr, Waiting* waiting = nullptr, const QuantWeight* wq = nullptr)
 {
     const int d_out = (int)d->d_out, d_in = (int)d->d_in, r = (int)d->r;
     if (d->s == 0.f) {  // scale-is-zero fast path: no U, no G
@@ -422,8 +425,10 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
         const int dt = dt_of(d->dtype);
         // past that rank B no longer fits the registers of a workgroup
         if (r <= NORM_ROWS_MAX_RANK) {
-            const NormRowsArgs a{(const bf16_t*)W, (const bf16_t*)A, (const bf16_t*)B, d_out, d_in, r, n.slices, n.tiles_per_slice, n.part};
-            DORA_HIP(launch_norm_rows(a, dt, st));
+            const bool codes = wq && norm_of_codes(d);
+            const NormRowsArgs a{(const bf16_t*)W, (const bf16_t*)A, (const bf16_t*)B, d_out, d_in, r, n.slices, n.tiles_per_slice, n.part,
+                                 codes ? *wq : QuantWeight{}};
+            DORA_HIP(codes ? launch_norm_quant(a, dt, st) : launch_norm_rows(a, dt, st));
             if (G_out) {
                 Seg sg{A, d_in, A, d_in, d_in};
                 GemmArgs g = bf16_args(dt, true, true, r, r, &sg, 1, 1.f, n.gram_p, r, true, 0);
@@ -713,7 +718,7 @@ size_t dora_workspace_bytes(const dora_desc* desc, int phase)
         case DORA_PHASE_BACKWARD_RECOMPUTE: { BwdPlan p; plan_bwd(desc, b, p, true, true, true); break; }
         case DORA_PHASE_FORWARD_DROPOUT: { FwdPlan p; plan_fwd(desc, b, p, true, true, true, true, true); break; }
         case DORA_PHASE_BACKWARD_DROPOUT: { BwdPlan p; plan_bwd(desc, b, p, true, true, true, true); break; }
-        case DORA_PHASE_NORM_QUANT: { NormPlan n; take_weight(desc, b); plan_norm(desc, b, n); break; }
+        case DORA_PHASE_NORM_QUANT: { NormPlan n; if (!norm_of_codes(desc)) take_weight(desc, b); plan_norm(desc, b, n); break; }
         case DORA_PHASE_FORWARD_QUANT: { FwdPlan p; take_weight(desc, b); plan_fwd(desc, b, p, true, true, true, true, true, true); break; }
         case DORA_PHASE_BACKWARD_QUANT: { BwdPlan p; take_weight(desc, b); plan_bwd(desc, b, p, true, true, true, true); break; }
         default: return 0;
@@ -900,7 +905,7 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     // over 4 bits the streaming launch is the faster one wherever it runs; it takes the weight as it is
     const bool streamed = !dropout && (wq ? quant_tokens(desc) : few_tokens(desc, one_product));
     const bool tiled = wq && !dropout && quant_tile(desc) && quant_tile_takes(*wq);
-    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && !streamed && !tiled));
+    const bool need_weight = wq && ((need_norm && !norm_of_codes(desc)) || (desc->tokens > 0 && !streamed && !tiled));
     if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     FwdPlan p;
@@ -925,7 +930,7 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     Waiting waiting;          // Eq. 5 and 6: g is read by the last launch of the tiled routes only
     if (need_norm) {
         float* cw = w_norm_out ? w_norm_out : p.c;
-        if ((st = norm_impl(desc, W, A, B, cw, p.norm, s, nullptr, nullptr, nullptr, &mag, T > 0 && !streamed ? &waiting : nullptr)) != DORA_OK)
+        if ((st = norm_impl(desc, W, A, B, cw, p.norm, s, nullptr, nullptr, nullptr, &mag, T > 0 && !streamed ? &waiting : nullptr, wq)) != DORA_OK)
             return st;
         c = cw;
     } else if (w_norm_out && w_norm_out != w_norm) {
@@ -1099,7 +1104,7 @@ static dora_status backward_impl(const dora_desc* desc, const void* dy, const vo
     const bool need_inner = (dm != nullptr) && (saved_inner == nullptr);
     const bool need_h = (saved_h == nullptr) && (dB != nullptr || need_inner);
     const bool need_dzb = dropout && (dx_lora != nullptr);
-    const bool need_weight = wq && (need_norm || (desc->tokens > 0 && (need_inner || dx || need_dzb)));
+    const bool need_weight = wq && ((need_norm && !norm_of_codes(desc)) || (desc->tokens > 0 && (need_inner || dx || need_dzb)));
     if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     BwdPlan p;
@@ -1121,7 +1126,7 @@ static dora_status backward_impl(const dora_desc* desc, const void* dy, const vo
     const float* c = w_norm;
     Waiting waiting;          // Eq. 5 and 6 up to the first reader of g, dm's second stage up to the end
     if (need_norm) {
-        if ((st = norm_impl(desc, W, A, B, p.c, p.norm, s, nullptr, nullptr, nullptr, &mag, &waiting)) != DORA_OK) return st;
+        if ((st = norm_impl(desc, W, A, B, p.c, p.norm, s, nullptr, nullptr, nullptr, &mag, &waiting, wq)) != DORA_OK) return st;
         c = p.c;
     }
     const bool mag_in_compose = !mag.done && !need_inner;   // then the compose backward is the only reader of g
@@ -1286,16 +1291,17 @@ dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const v
     if (st != DORA_OK || (st = check_quant(desc, wq, w)) != DORA_OK) return st;
     DORA_REQ_PTR(A); DORA_REQ_PTR(B); DORA_REQ_PTR(w_norm);
     if (norm_refused(desc)) return DORA_ERR_SHAPE;
+    const bool read_back = !norm_of_codes(desc);
     Bump sizing(nullptr);
     NormPlan n;
-    take_weight(desc, sizing);
+    if (read_back) take_weight(desc, sizing);
     plan_norm(desc, sizing, n);
     if ((st = check_ws(ws, ws_bytes, sizing.off)) != DORA_OK) return st;
     Bump b(ws);
-    void* const W = take_weight(desc, b);
+    void* const W = read_back ? take_weight(desc, b) : nullptr;
     plan_norm(desc, b, n);
-    DORA_HIP(launch_dequantize(desc->dtype, w, W, (hipStream_t)stream));
-    return norm_impl(desc, W, A, B, w_norm, n, (hipStream_t)stream);
+    if (read_back) DORA_HIP(launch_dequantize(desc->dtype, w, W, (hipStream_t)stream));
+    return norm_impl(desc, W, A, B, w_norm, n, (hipStream_t)stream, nullptr, nullptr, nullptr, nullptr, nullptr, &w);
 }
 
 dora_status dora_forward_quant(const dora_desc* desc, const void* x, const void* x_lora, const dora_quant* wq, const void* A,
