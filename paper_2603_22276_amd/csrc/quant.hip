@@ -48,8 +48,7 @@ __device__ __forceinline__ uint32_t lanes_pair_max(uint32_t v, int lanes)
 // meet by lane exchanges, so a weight is read once (groups above 512: twice, the second time from the L2).  16-bit floats are
 // ordered as their bits are: the extremes are found two at a time, the largest positive as it is and the most negative as the largest
 // number with the sign bit; exponents of ones show infinities and NaN.  Bound: memory, and the vector instructions of rounding
-// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us,
-// 3.5 TB/s (65 with the extremes, the eight quotients and the eight codes of a thread one by one).
+// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us, 3.5 TB/s (65 with the extremes, the eight quotients and the eight codes of a thread one by one).
 //
 // Scales have four significant bits.  A symmetric code (at most 3 bits of odd part, 4 with a zero point) times such a scale
 // has 8 at most, so the weight that codes and scale stand for is a bf16 and an fp16 number without rounding, and every path
@@ -120,11 +119,12 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
     }
     const bool some = s > 0.f;                         // neither 0 nor NaN: otherwise the code of 0 everywhere
     // w / s is the product with 1 / s and one correction by its remainder, which is exact: the quotient rounded to nearest, a tie
-    // between two codes among them.
-    const float inv = some ? 1.f / s : 0.f;
-    auto over_s = [&](float v) { const float t = v * inv; return fmaf(fmaf(-t, s, v), inv, t); };
+    // between two codes among them.  Scales whose reciprocal or remainders would leave the normal range are lifted with their weights.
+    const bool tiny = !std::is_same<T, f16_t>::value && some && s < 0x1p-100f;
+    const float by = tiny ? s * 0x1p100f : s, inv = some ? 1.f / by : 0.f;
+    auto over_s = [&](float v) { const float t = v * inv; return fmaf(fmaf(-t, by, v), inv, t); };
     const float most = std::is_same<T, f16_t>::value && some ? floorf(over_s(65504.f)) : 15.f;
-    if constexpr (ZERO) z = some ? fminf(fmaxf(rintf(over_s(-lo)), 0.f), 15.f) : 0.f;
+    if constexpr (ZERO) z = some ? fminf(fmaxf(rintf(over_s(tiny ? -lo * 0x1p100f : -lo)), 0.f), 15.f) : 0.f;
     if (first) {
         V::put(p.scale, at, s);
         if constexpr (ZERO) V::put(p.zero, at, z);
@@ -132,6 +132,10 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
     const float offset = ZERO ? z : 8.f, least = fmaxf(-offset, -most), largest = fminf(15.f - offset, most);
     for (int k = k_first; k < k_end; k += 512) {
         if (group > 512) V::load(src + k, f);
+        if (tiny) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= 0x1p100f;
+        }
         uint32_t word = 0;
         float t[8];
 #pragma unroll

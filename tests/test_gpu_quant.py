@@ -89,6 +89,25 @@ def test_groups_of_zeros_infinities_and_tiny_weights(dtype, kind):
     assert np.isfinite(back[4]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("group", [32, 2048])
+@pytest.mark.parametrize("exponent", [-126, -122, -116, -104, -96])
+def test_tiny_weights_take_the_nearest_code(dtype, kind, group, exponent):
+    W = U.stored(np.random.default_rng(-exponent).uniform(-1, 1, (8, 2048)) * 2.0 ** exponent, dtype)
+    q, scale, zero, back = quantize_on_gpu(W, dtype, kind, group)
+    s = np.repeat(scale, group, axis=1)[:, :2048]
+    if kind == "fp4":
+        values = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+        values = np.concatenate([values, -values])
+    else:
+        values = np.arange(16.0)
+    off = 8.0 * (kind == "int4") if zero is None else np.repeat(zero, group, axis=1)[:, :2048]
+    best = np.min([np.abs((v - off) * s - W) for v in values], axis=0)
+    # (read back the product is rounded once: half a step of the smallest numbers)
+    assert np.all(np.abs(back - W) <= best * (1 + 2.0 ** -20) + (2.0 ** -134 if dtype == "bf16" else 2.0 ** -150))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("kind", KINDS)
 def test_any_scale_reads_back_within_half_a_step(dtype, kind):
