@@ -198,8 +198,9 @@ struct NormRowsArgs {
     const bf16_t* b;        // [d_out, r]
     int d_out, d_in, r;
     int slices, tiles_per_slice;   // slices of tiles_per_slice column tiles of 128 each; none of them empty
-    float* part;            // [3][slices][d_out]: base_sq, cross, ba_sq
+    float* part;            // [3][slices][d_out]: base_sq, cross, ba_sq; over codes [slices][d_out], the sum of (w + s v)^2
     QuantWeight q;          // instead of w: d_in a multiple of 32
+    float s;                // with q
 };
 hipError_t launch_norm_rows(const NormRowsArgs& a, int dt, hipStream_t st);
 hipError_t launch_norm_quant(const NormRowsArgs& a, int dt, hipStream_t st);   // (norm_quant.hip)

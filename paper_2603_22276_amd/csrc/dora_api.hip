@@ -427,7 +427,7 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
         if (r <= NORM_ROWS_MAX_RANK) {
             const bool codes = wq && norm_of_codes(d);
             const NormRowsArgs a{(const bf16_t*)W, (const bf16_t*)A, (const bf16_t*)B, d_out, d_in, r, n.slices, n.tiles_per_slice, n.part,
-                                 codes ? *wq : QuantWeight{}};
+                                 codes ? *wq : QuantWeight{}, d->s};
             DORA_HIP(codes ? launch_norm_quant(a, dt, st) : launch_norm_rows(a, dt, st));
             if (G_out) {
                 Seg sg{A, d_in, A, d_in, d_in};
@@ -437,8 +437,9 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
                 DORA_HIP(launch_gram_reduce(n.gram_p, n.ks_g, r, G_out, nullptr, nullptr, dt, st));
             }
             const size_t all = (size_t)n.slices * d_out;
-            const NormFinalArgs fin = norm_final_args(base_sq ? base_sq : n.part, base_sq ? 1 : n.slices, n.part + all, n.slices,
-                                                      n.part + 2 * all, n.slices, (double)d->s, c, terms, d_out, mag ? mag->m : nullptr,
+            const int low = codes ? 0 : n.slices;      // (over codes one sum holds all three)
+            const NormFinalArgs fin = norm_final_args(base_sq ? base_sq : n.part, base_sq ? 1 : n.slices, n.part + all, low,
+                                                      n.part + 2 * all, low, codes ? 0.0 : (double)d->s, c, terms, d_out, mag ? mag->m : nullptr,
                                                       mag ? mag->eps : 0.f, mag ? mag->g : nullptr, mag ? mag->gm1 : nullptr);
             if (waiting) { waiting->norm = true; waiting->norm_args = fin; }
             else DORA_HIP(launch_norm_final(fin, st));

@@ -3,6 +3,8 @@
 //
 //   base[m] = sum_n W[m,n]^2,   cross[m] = sum_n W[m,n] V[m,n],   ba[m] = sum_n V[m,n]^2,   V = B A
 //
+// or, over codes, where nobody asks for the terms, the one sum (W[m,n] + s V[m,n])^2 that they make: two vector instructions less an element.
+//
 // V lives in the accumulators of one 128 x 128 tile at a time and is never stored.  Its products are as many as those of
 // U = W A^T (2 d_out d_in r), but W meets V element by element, so the Gram matrix, B G and the launches between them are not
 // needed for the norm, and both low-rank sums come from fp32 values.
@@ -197,45 +199,34 @@ struct Scale {
         by = Elem16<DT>::lo(scale);
         less = WK == W_INT4 ? -(zeros ? Elem16<DT>::lo(zero) : 8.f) * by : 0.f;
     }
-    template <int WK, int C>
-    __device__ __forceinline__ float value(uint32_t codes) const
-    {
-        // (the byte 0q read as E4M3 is q / 512: two columns to a conversion)
-        if constexpr (WK == W_INT4)
-            return fmaf(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8((C % 2 ? codes >> 4 : codes) & 0x0f0fu, 512.f, false)[C / 2], by, less);
-        else return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, C / 2)[C % 2] * by;
-    }
 };
-// element C of four
-template <int WK, int DT, int C>
-__device__ __forceinline__ float value_of(typename Four<WK>::raw_t w, const Scale& s)
+// code C of four as a float (the byte 0q read as E4M3 is q / 512: two columns to a conversion either way)
+template <int WK, int C>
+__device__ __forceinline__ float code_of(uint32_t codes)
 {
-    if constexpr (WK == W_16) {
-        const uint32_t w2 = __builtin_bit_cast(u32x2_t, w)[C / 2];
-        return C % 2 ? Elem16<DT>::hi(w2) : Elem16<DT>::lo(w2);
-    } else {
-        return s.value<WK, C>(w);
-    }
+    if constexpr (WK == W_INT4) return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((C % 2 ? codes >> 4 : codes) & 0x0f0fu, 512.f, false)[C / 2];
+    else return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, C / 2)[C % 2];
 }
 
 // a workgroup's sums leave: over the four lanes and two waves that share a row
-__device__ __forceinline__ void store_sums(const NormRowsArgs& p, float* red, const float (&sum)[3][4], int wave, int lane, int slice,
+template <int SUMS>
+__device__ __forceinline__ void store_sums(const NormRowsArgs& p, float* red, const float (&sum)[SUMS][4], int wave, int lane, int slice,
                                            int m0, int rows)
 {
-    __syncthreads();                                   // red: [2 halves of the columns][3][BM]
+    __syncthreads();                                   // red: [2 halves of the columns][SUMS][BM]
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < SUMS; ++k) {
             float v = sum[k][i];
             v += __shfl_xor(v, 16);
             v += __shfl_xor(v, 32);
-            if (lane < 16) red[((wave & 1) * 3 + k) * BM + (wave >> 1) * 64 + i * 16 + lane] = v;
+            if (lane < 16) red[((wave & 1) * SUMS + k) * BM + (wave >> 1) * 64 + i * 16 + lane] = v;
         }
     __syncthreads();
-    for (int e = threadIdx.x; e < 3 * BM; e += 256) {
+    for (int e = threadIdx.x; e < SUMS * BM; e += 256) {
         const int k = e / BM, m = e % BM;
-        if (m < rows) p.part[((int64_t)k * p.slices + slice) * p.d_out + m0 + m] = red[e] + red[3 * BM + e];
+        if (m < rows) p.part[((int64_t)k * p.slices + slice) * p.d_out + m0 + m] = red[e] + red[SUMS * BM + e];
     }
 }
 
@@ -276,9 +267,10 @@ __global__ __launch_bounds__(256, 2) void norm_rows_kernel(NormRowsArgs p)
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lds_cptr_t)smem;
     read_offsets<WK>(smem_lds, wave, lane, rb, rwd);
     const uint32_t rs_at = smem_lds + (uint32_t)(wave * 256 + l16 * 4);   // codes: the scale of a lane's row, relative to the slot
-    float sum[3][4];
+    constexpr int SUMS = WK == W_16 ? 3 : 1;
+    float sum[SUMS][4];
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
+    for (int k = 0; k < SUMS; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[k][i] = 0.f;
     int cur = 0;                                       // slot of the step under way; the one before it is refilled
@@ -355,20 +347,29 @@ __global__ __launch_bounds__(256, 2) void norm_rows_kernel(NormRowsArgs p)
             static_for<2>([&](auto iit) {
                 constexpr int ii = decltype(iit)::value, i = h * 2 + ii;
                 // the sixteen products of a block first, then the running sum over tiles
-                float tb = 0.f, tc = 0.f, ta = 0.f;
-                Scale sc[2];
-                if constexpr (WK != W_16) {
+                if constexpr (WK == W_16) {
+                    float tb = 0.f, tc = 0.f, ta = 0.f;
+                    static_for<16>([&](auto et) {
+                        constexpr int j = decltype(et)::value / 4, e = decltype(et)::value % 4;
+                        const uint32_t w2 = __builtin_bit_cast(u32x2_t, w[ii * 4 + j])[e / 2];
+                        const float wv = e % 2 ? E::hi(w2) : E::lo(w2), v = acc[i][j][e];
+                        tb = fmaf(wv, wv, tb);
+                        tc = fmaf(wv, v, tc);
+                        ta = fmaf(v, v, ta);
+                    });
+                    sum[0][i] += tb; sum[1][i] += tc; sum[2][i] += ta;
+                } else {
+                    Scale sc[2];
                     sc[0].set<WK, DT>(sr[2 * ii], zr[2 * ii], p.q.zero != nullptr);
                     sc[1].set<WK, DT>(sr[2 * ii + 1], zr[2 * ii + 1], p.q.zero != nullptr);
+                    float t = 0.f;
+                    static_for<16>([&](auto et) {
+                        constexpr int j = decltype(et)::value / 4, e = decltype(et)::value % 4;
+                        const float u = fmaf(code_of<WK, e>(w[ii * 4 + j]), sc[j / 2].by, fmaf(p.s, acc[i][j][e], sc[j / 2].less));
+                        t = fmaf(u, u, t);
+                    });
+                    sum[0][i] += t;
                 }
-                static_for<16>([&](auto et) {
-                    constexpr int j = decltype(et)::value / 4, e = decltype(et)::value % 4;
-                    const float wv = value_of<WK, DT, e>(w[ii * 4 + j], sc[j / 2]), v = acc[i][j][e];
-                    tb = fmaf(wv, wv, tb);
-                    tc = fmaf(wv, v, tc);
-                    ta = fmaf(v, v, ta);
-                });
-                sum[0][i] += tb; sum[1][i] += tc; sum[2][i] += ta;
             });
             cur = cur + 1 == NS ? 0 : cur + 1;
         });
@@ -478,9 +479,10 @@ __global__ __launch_bounds__(256, 1) void norm_rows_deep_kernel(NormRowsArgs p)
     uint32_t rb[4], rwd[4];
     read_offsets<WK>(smem_lds, wave, lane, rb, rwd);
     const uint32_t rs_at = smem_lds + (uint32_t)(wave * 256 + l16 * 4);   // codes: the scale of a lane's row, relative to the slot
-    float sum[3][4], part[3];                          // base, cross, ba of the four row blocks; of one block in one tile
+    constexpr int SUMS = WK == W_16 ? 3 : 1;
+    float sum[SUMS][4], part[SUMS];                    // base, cross, ba of the four row blocks; of one block in one tile
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < SUMS; ++k) {
         part[k] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[k][i] = 0.f;
@@ -491,21 +493,31 @@ __global__ __launch_bounds__(256, 1) void norm_rows_deep_kernel(NormRowsArgs p)
     for (int i = 0; i < 4; ++i) sr[i][0] = sr[i][1] = zr[i][0] = zr[i][1] = 0u;
     Scale sc;
     f32x4_t old[4][4];
-    // Instruction u of the sums over the products in `old` and W's in w: four to an element, whose order is row block, column
-    // block, column.  The sixteen elements of a block first, then the running sum over tiles.
+    // Instruction u of the sums over the products in `old` and W's in w: four (codes: three) to an element, whose order is row block,
+    // column block, column.  The sixteen elements of a block first, then the running sum over tiles.
+    constexpr int PER = WK == W_16 ? 4 : 3;
     float wv = 0.f;
     const bool zeros = WK == W_INT4 && p.q.zero != nullptr;
     auto sums = [&](auto u_tag) {
-        constexpr int u = decltype(u_tag)::value, e = u / 4, i = e / 16, j = e / 4 % 4, c = e % 4;
+        constexpr int u = decltype(u_tag)::value, e = u / PER, i = e / 16, j = e / 4 % 4, c = e % 4;
         const float v = old[i][j][c];
-        if constexpr (WK != W_16 && u % 32 == 0) sc.set<WK, DT>(sr[i][j / 2], zr[i][j / 2], zeros);
-        if constexpr (u % 4 == 0) wv = value_of<WK, DT, c>(w[i][j], sc);
-        if constexpr (u % 4 == 1) part[0] = fmaf(wv, wv, e % 16 ? part[0] : 0.f);
-        if constexpr (u % 4 == 2) part[1] = fmaf(wv, v, e % 16 ? part[1] : 0.f);
-        if constexpr (u % 4 == 3) part[2] = fmaf(v, v, e % 16 ? part[2] : 0.f);
-        if constexpr (u % 64 == 63) {
+        if constexpr (WK == W_16) {
+            if constexpr (u % 4 == 0) {
+                const uint32_t w2 = __builtin_bit_cast(u32x2_t, w[i][j])[c / 2];
+                wv = c % 2 ? E::hi(w2) : E::lo(w2);
+            }
+            if constexpr (u % 4 == 1) part[0] = fmaf(wv, wv, e % 16 ? part[0] : 0.f);
+            if constexpr (u % 4 == 2) part[1] = fmaf(wv, v, e % 16 ? part[1] : 0.f);
+            if constexpr (u % 4 == 3) part[2] = fmaf(v, v, e % 16 ? part[2] : 0.f);
+        } else {
+            if constexpr (u % (8 * PER) == 0) sc.set<WK, DT>(sr[i][j / 2], zr[i][j / 2], zeros);
+            if constexpr (u % 3 == 0) wv = fmaf(p.s, v, sc.less);
+            if constexpr (u % 3 == 1) wv = fmaf(code_of<WK, c>(w[i][j]), sc.by, wv);
+            if constexpr (u % 3 == 2) part[0] = fmaf(wv, wv, e % 16 ? part[0] : 0.f);
+        }
+        if constexpr (u % (16 * PER) == 16 * PER - 1) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) sum[k][i] += part[k];
+            for (int k = 0; k < SUMS; ++k) sum[k][i] += part[k];
         }
     };
     auto read_w = [&](auto n_tag, uint32_t slot0, uint32_t slot1) {    // rows 16 (n / 4) .. of the wave, column block n % 4
@@ -585,7 +597,7 @@ __global__ __launch_bounds__(256, 1) void norm_rows_deep_kernel(NormRowsArgs p)
                     walk.template issue_one<seq, k % LPS>(t, smem + behind((seq - s) % NS) * SLOT);
                 }
                 if constexpr (OLD && h > 0) {
-                    constexpr int N = (2 * S - 1) * 16, m = (h - 1) * 16 + n, u0 = m * 256 / N, u1 = (m + 1) * 256 / N;
+                    constexpr int N = (2 * S - 1) * 16, m = (h - 1) * 16 + n, u0 = m * (64 * PER) / N, u1 = (m + 1) * (64 * PER) / N;
                     static_for<u1 - u0>([&](auto ut) { sums(std::integral_constant<int, u0 + decltype(ut)::value>{}); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -610,7 +622,7 @@ __global__ __launch_bounds__(256, 1) void norm_rows_deep_kernel(NormRowsArgs p)
 #pragma unroll
     for (int q = 0; q < 2; ++q) asm volatile("" : "+v"(frag[q][0]), "+v"(frag[q][1]), "+v"(frag[q][2]), "+v"(frag[q][3]));
     __builtin_amdgcn_sched_barrier(0);
-    static_for<256>([&](auto ut) { sums(ut); });
+    static_for<64 * PER>([&](auto ut) { sums(ut); });
     wait_vmcnt<0>();                                   // the loads past the end have written their zeros
     store_sums(p, reinterpret_cast<float*>(smem), sum, wave, lane, walk.slice, walk.m0, rows);
 }
