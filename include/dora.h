@@ -237,8 +237,8 @@ dora_status dora_backward(const dora_desc* desc, const void* dy, const void* x, 
 
 /*
  * The module under LoRA dropout (App. B "Chunked dropout path"): the adapter branch sees its own input
- * x_lora = dropout(x), formed by the caller (device, const, `dtype` [tokens, d_in]; the library draws no
- * random numbers), while the frozen layer's output stays that of x.  The compose then runs on the adapter
+ * x_lora = dropout(x), formed by the caller (device, const, `dtype` [tokens, d_in]; these calls draw no
+ * random numbers, dora_dropout does), while the frozen layer's output stays that of x.  The compose then runs on the adapter
  * branch's own base:
  *   y = x W^T + delta,   delta = (g-1) (.) (x_lora W^T) + g (.) (s * (x_lora A^T) B^T)  [+ bias]
  * i.e. delta = x_lora (W' - W)^T with W' the adapted weight of Eq. 1; h and inner are those of x_lora.
@@ -246,7 +246,7 @@ dora_status dora_backward(const dora_desc* desc, const void* dy, const void* x, 
  * [tokens, d_out] scratch tensor inside the workspace, DORA_PHASE_FORWARD_DROPOUT.)
  * Backward, norm constant:  dx = dy W (frozen path),  dx_lora = ((g-1) (.) dy) W + dh A,  dh = s (g (.) dy) B,
  * dA = dh^T x_lora,  dB = s (g (.) dy)^T h,  dm = (sum_t dy * inner) / max(w_norm, eps); the caller applies
- * its dropout mask to dx_lora and adds it to dx (dx_lora may lie over dy).  dx, dx_lora, dA, dB, dm may each be NULL.  saved_h /
+ * its dropout mask to dx_lora and adds it to dx (as dora_dropout_backward does; dx_lora may lie over dy).  dx, dx_lora, dA, dB, dm may each be NULL.  saved_h /
  * saved_inner as written by dora_forward_dropout, or NULL (recomputed from x_lora).  With x_lora == x the
  * results are those of dora_forward / dora_backward (dx + dx_lora = dx of the plain module).
  */
@@ -287,8 +287,8 @@ typedef struct {
  *     INT4 with zero     : over the group and 0, scale = (max - min) / 15, zero = round(-min / scale), q = zero + round(w / scale).
  *     FP4                : scale = max|w| / 6, q the nearest E2M1 float to w / scale, halfway to the even code.
  *   Scales are rounded to four significant bits (to nearest; with a zero point upwards), so that a weight read back is a
- *   bf16 or fp16 number without rounding.  Codes are kept in range, in fp16 also so that no weight reads back as an infinity; a group whose scale is 0 reads back as 0, one that
- *   holds an infinity or NaN has scale NaN and reads back as NaN.
+ *   bf16 or fp16 number without rounding.  Codes are kept in range, in fp16 also so that no weight reads back as an infinity; a
+ *   group whose scale is 0 reads back as 0, one that holds an infinity or NaN has scale NaN and reads back as NaN.
  * dora_dequantize : W [d_out, d_in] `dtype` out, rounded once.
  * r and tokens of desc are not read.  Neither needs a workspace.
  */
@@ -304,7 +304,8 @@ dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W
  * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  In 16 bits the norm (s != 0, r <= 384,
  * d_in a multiple of 32) and the plain forward of up to 320 tokens take the codes as they are, the latter within limits of shape; everything
  * else reads W back into the workspace in the storage type first (2 or 4 bytes a weight).  Either way a product sees each weight
- * rounded at most once, which scales of up to four significant bits and zero points of 0 to 15 do not show.
+ * rounded at most once, which scales of up to four significant bits and zero points of 0 to 15 do not show.  An infinity in a
+ * row of x makes that row of y infinite or NaN.
  */
 dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const void* A, const void* B, float* w_norm, void* ws,
                             size_t ws_bytes, void* stream);
