@@ -241,6 +241,22 @@ void norm_slices(int64_t d_out, int64_t d_in, int64_t r, size_t fixed_bytes, siz
     }
 }
 
+// The same over codes up to r 128, whose tiles cost vector instructions: 3500 cycles with a CU to itself, 5300 each where two workgroups
+// share one, and as much more before the first.  In: the slices of the 16-bit weight, whose scratch has room for three sums of each.
+// (us with 256 workgroups / 512, codes in cache: 4096 x 4096, r 64 10.9 / 11.7, r 128 13.9 / 14.9; 8192 x 8192, r 64 28.5 / 24.9; 14336
+// x 4096, r 64, 224 / 448 workgroups 27.9 / 23.7.)
+void norm_code_slices(int64_t d_out, int64_t d_in, int64_t r, int& slices, int& tiles_per_slice)
+{
+    if (r > 128) return;
+    const int64_t blocks = (d_out + TILE - 1) / TILE, tiles = (d_in + TILE - 1) / TILE, most = std::min<int64_t>(tiles, 3 * (int64_t)slices);
+    int64_t best = -1;
+    for (int64_t n = 1; n <= most; ++n) {
+        const int64_t per = (tiles + n - 1) / n, used = (tiles + per - 1) / per, wgs = blocks * used;
+        const int64_t cost = (wgs <= 256 ? per * 3500 + 8000 : (wgs + 511) / 512 * (per * 5300 + 13300)) + used * 50;
+        if (best < 0 || cost < best) { best = cost; slices = (int)used; tiles_per_slice = (int)per; }
+    }
+}
+
 // fp32 norm: rows of a workgroup (one or two blocks of 16) and slices of the columns, the cheapest in tenths of a microsecond.  A
 // CU has one workgroup of sixteen waves; a wave takes groups of 32 columns, and 64 of the rank take it 1 us (1.6 with 32 rows) with
 // a SIMD to itself and 3.5 (5.9) where four share one; with 16 rows it takes the rank in pieces of 64, whose last one costs two
@@ -426,7 +442,9 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
         // past that rank B no longer fits the registers of a workgroup
         if (r <= NORM_ROWS_MAX_RANK) {
             const bool codes = wq && norm_of_codes(d);
-            const NormRowsArgs a{(const bf16_t*)W, (const bf16_t*)A, (const bf16_t*)B, d_out, d_in, r, n.slices, n.tiles_per_slice, n.part,
+            int slices = n.slices, tiles_per_slice = n.tiles_per_slice;
+            if (codes) norm_code_slices(d_out, d_in, r, slices, tiles_per_slice);
+            const NormRowsArgs a{(const bf16_t*)W, (const bf16_t*)A, (const bf16_t*)B, d_out, d_in, r, slices, tiles_per_slice, n.part,
                                  codes ? *wq : QuantWeight{}, d->s};
             DORA_HIP(codes ? launch_norm_quant(a, dt, st) : launch_norm_rows(a, dt, st));
             if (G_out) {
@@ -436,9 +454,9 @@ dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const vo
                 DORA_HIP(launch_gemm_bf16(g, DORA_K_GRAM, st));
                 DORA_HIP(launch_gram_reduce(n.gram_p, n.ks_g, r, G_out, nullptr, nullptr, dt, st));
             }
-            const size_t all = (size_t)n.slices * d_out;
-            const int low = codes ? 0 : n.slices;      // (over codes one sum holds all three)
-            const NormFinalArgs fin = norm_final_args(base_sq ? base_sq : n.part, base_sq ? 1 : n.slices, n.part + all, low,
+            const size_t all = (size_t)slices * d_out;
+            const int low = codes ? 0 : slices;      // (over codes one sum holds all three)
+            const NormFinalArgs fin = norm_final_args(base_sq ? base_sq : n.part, base_sq ? 1 : slices, n.part + all, low,
                                                       n.part + 2 * all, low, codes ? 0.0 : (double)d->s, c, terms, d_out, mag ? mag->m : nullptr,
                                                       mag ? mag->eps : 0.f, mag ? mag->g : nullptr, mag ? mag->gm1 : nullptr);
             if (waiting) { waiting->norm = true; waiting->norm_args = fin; }
