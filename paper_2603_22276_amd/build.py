@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdora.so")
 SOURCES = ["dora_api.hip", "gemm_bf16.hip", "few_tokens.hip", "norm_rows.hip", "norm_quant.hip", "elementwise.hip", "sgemm_f32.hip", "probes.hip",
-           "quant.hip", "quant_tokens.hip", "quant_tile.hip", "dropout.hip"]
+           "quant.hip", "quant_tokens.hip", "quant_tile.hip", "project_tokens.hip", "dropout.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -371,6 +371,15 @@ struct QuantTokensArgs {
 };
 hipError_t launch_quant_tokens(const QuantTokensArgs& a, int dt, hipStream_t st);
 
+// h = x A^T of a few hundred tokens (project_tokens.hip); hs != nullptr: s h as well, from the same sums
+struct ProjectTokensArgs {
+    const bf16_t *x, *a;      // [T, d_in], [r, d_in]
+    int T, d_in, r;
+    float s;
+    bf16_t *h, *hs;           // [T, r]
+};
+hipError_t launch_project_tokens(const ProjectTokensArgs& a, int dt, hipStream_t st);
+
 // forward of more tokens over such a weight (quant_tile.hip): h is there; part != nullptr: the sums of each slice of the columns
 // instead of y and inner
 struct QuantTileArgs {

@@ -551,10 +551,16 @@ inline bool quant_tokens(const dora_desc* d)
 }
 
 // and of more tokens, as long as decoding in the product costs less than reading the weight back (us, read back / decoded, weights
-// from memory: 33 tokens 1024 x 4096, r 64 32 / 26, 64 tokens 14336 x 4096 89 / 49, 256 tokens 4096 x 4096 48 / 46, 8192 x 8192 91 /
+// from memory, h in slices in both: 33 tokens 1024 x 4096, r 64 32 / 26, 64 tokens 14336 x 4096 89 / 49, 256 tokens 4096 x 4096 48 / 46, 8192 x 8192 91 /
 // 76, 27648 x 5120 210 / 111; 384 tokens 53 / 53 and 103 / 106 at the first two of these, 1024 tokens 63 / 78).
 constexpr int64_t QUANT_TILE_MAX = 320;
 inline bool quant_tile(const dora_desc* d) { return is16(d->dtype) && d->tokens > 32 && d->tokens <= QUANT_TILE_MAX; }
+
+// h in one launch in front of such a product (project_tokens.hip), while every tile of 16 x 16 has a CU to itself and its columns take it a
+// round of loads and a quarter (us of a forward, sliced / this: 1024 x 4096, r 64, 33 tokens 26.4 / 24.5; 4096 x 4096, r 384, 128
+// tokens 41.0 / 36.0, 200 tokens, 312 tiles, 47.7 / 49.3; 3000 x 2056, r 72, 333 tokens 40.5 / 33.9; 5120 x 5120, r 128, 256 tokens 54.9 /
+// 52.8; 8192 x 8192, r 64, 64 tokens 45.0 / 47.5).
+inline bool project_tokens(const dora_desc* d) { return is16(d->dtype) && d->d_in <= 5120 && (d->tokens + 15) / 16 * ((d->r + 15) / 16) <= 256; }
 
 // scratch for the K slices of a [tokens, n] product over k whose N-side operand has rows of ldb
 inline size_t slice_floats(const dora_desc* d, int64_t n, int64_t k, int64_t ldb)
@@ -962,7 +968,9 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     void* h = saved_h ? saved_h : p.h;
     if (tiled) {
         Seg s1{x, d_in, A, d_in, d_in};
-        DORA_HIP(contract(desc->dtype, true, true, T, r, &s1, 1, 1.f, h, r, false, DORA_K_GEMM_H, s, p.skp, nullptr, 0.f, &waiting));
+        const ProjectTokensArgs pt{(const bf16_t*)x, (const bf16_t*)A, T, d_in, r, 0.f, (bf16_t*)h, nullptr};
+        if (project_tokens(desc)) DORA_HIP(launch_project_tokens(pt, dt_of(desc->dtype), s));
+        else DORA_HIP(contract(desc->dtype, true, true, T, r, &s1, 1, 1.f, h, r, false, DORA_K_GEMM_H, s, p.skp, nullptr, 0.f, &waiting));
         DORA_HIP(launch_waiting(waiting, s));
         const int ks = quant_tile_slices(T, *wq);
         const QuantTileArgs q{(const bf16_t*)x, T, *wq, (const bf16_t*)h, r, (const bf16_t*)B, desc->s, eff_eps(desc), m, c, (const bf16_t*)bias,
@@ -976,7 +984,9 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     if (one_product) {
         // h = x A^T, written twice from the same accumulators: as it is (the saved tensor) and scaled by s
         Seg s1{x, d_in, A, d_in, d_in};
-        DORA_HIP(contract(desc->dtype, true, true, T, r, &s1, 1, 1.f, h, r, false, DORA_K_GEMM_H, s, p.skp, p.hs, desc->s, &waiting));
+        const ProjectTokensArgs pt{(const bf16_t*)x, (const bf16_t*)A, T, d_in, r, desc->s, (bf16_t*)h, (bf16_t*)p.hs};
+        if (wq && project_tokens(desc)) DORA_HIP(launch_project_tokens(pt, dt_of(desc->dtype), s));
+        else DORA_HIP(contract(desc->dtype, true, true, T, r, &s1, 1, 1.f, h, r, false, DORA_K_GEMM_H, s, p.skp, p.hs, desc->s, &waiting));
         DORA_HIP(launch_waiting(waiting, s));
         GemmArgs g = inner_product(desc, x, W, B, p.hs);
         g.epilogue = EPI_COMPOSE;

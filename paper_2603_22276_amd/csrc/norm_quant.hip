@@ -6,8 +6,8 @@
 // Bound: the matrix cores from r about 200 on (8192 x 8192, r 384: 52 GFLOP, 0.9 PFLOP/s of them in the launch); below, the vector
 // instructions of the sum, about 350 to the 32 S matrix instructions of a wave's tile.  Against reading the weight back first and forming
 // the three sums over that, and against the three sums over codes, us of a norm with Eq. 5, weights from memory: 8192 x 8192, r 384
-// 97 / 73 / 66, r 64 60 / 31 / 28; 4096 x 4096, r 384 36 / 24 / 20, r 64 13 in the end; 1024 x 4096, r 64 15.7 / 9.5 / 7.8; 27648 x 5120, r 384 195 / 142 /
-// 134.
+// 97 / 73 / 66, r 64 60 / 31 / 28; 4096 x 4096, r 384 36 / 24 / 20; 1024 x 4096, r 64 15.7 / 9.5 / 7.8; 27648 x 5120, r 384 195 /
+// 142 / 134.
 #include "norm_rows_body.hpp"
 
 namespace dora {
