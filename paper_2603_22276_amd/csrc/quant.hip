@@ -48,7 +48,8 @@ __device__ __forceinline__ uint32_t lanes_pair_max(uint32_t v, int lanes)
 // meet by lane exchanges, so a weight is read once (groups above 512: twice, the second time from the L2).  16-bit floats are
 // ordered as their bits are: the extremes are found two at a time, the largest positive as it is and the most negative as the largest
 // number with the sign bit; exponents of ones show infinities and NaN.  Bound: memory, and the vector instructions of rounding
-// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us, 3.5 TB/s (65 with the extremes, the eight quotients and the eight codes of a thread one by one).
+// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us, 3.5 TB/s (65 with the extremes, the eight quotients and the
+// eight codes of a thread one by one).
 //
 // Scales have four significant bits.  A symmetric code (at most 3 bits of odd part, 4 with a zero point) times such a scale
 // has 8 at most, so the weight that codes and scale stand for is a bf16 and an fp16 number without rounding, and every path

@@ -5,8 +5,9 @@
 // and token rows (buffer_load ... lds, no barrier: only its own vmcnt).  Codes become 16-bit integers (or E2M1 floats) exactly,
 // products are summed in fp32 within a group, and the group's sum is multiplied by the scale in fp32: no weight is rounded,
 // whatever the scale.  A zero point enters as the addend of the group's first MFMA, its negative times the sum of x over the group,
-// which one more MFMA against a constant gives for all rows (-8 times it where the zero point is the same everywhere).  Which columns a lane multiplies in a k-step is free as long as the x fragments take the same ones and a k-step stays
-// within a group: a lane's share of a group is consecutive, so it is one read of 16, 8 or 4 bytes of codes.
+// which one more MFMA against a constant gives for all rows (-8 times it where the zero point is the same everywhere).  Which columns
+// a lane multiplies in a k-step is free as long as the x fragments take the same ones and a k-step stays within a group: a lane's share
+// of a group is consecutive, so it is one read of 16, 8 or 4 bytes of codes.
 //
 // Codes and x straight from memory in the MFMA's own layout, without the LDS: sixteen lanes in a row then are sixteen rows, each
 // a line of its own to the L1 (14336 x 4096, r 8, 27 tokens, codes from memory 25 us, 20 this way).  Scales and zero points one at
