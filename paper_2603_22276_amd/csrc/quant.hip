@@ -106,8 +106,13 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
         }
     }
     float s, z = 0.f;
-    if constexpr (ZERO) s = four_bits_up((hi - lo) / 15.f);
-    else s = four_bits(fmaxf(hi, -lo) / (CODE == DORA_QUANT_INT4 ? 7.f : 6.f));
+    if constexpr (ZERO) {
+        // A span of finite weights may pass the largest float: half of it then, and the scale twice as large.
+        const float span = hi - lo;
+        const bool wide = !std::is_same<T, f16_t>::value && !(span <= 3.402823466e38f);
+        s = four_bits_up((wide ? 0.5f * hi - 0.5f * lo : span) / 15.f);
+        if (wide) s += s;
+    } else s = four_bits(fmaxf(hi, -lo) / (CODE == DORA_QUANT_INT4 ? 7.f : 6.f));
     // What is read back stays finite in fp16: 6 x 10240 is, and a code is not taken past 65504.
     if constexpr (std::is_same<T, f16_t>::value && CODE == DORA_QUANT_FP4) s = fminf(s, 10240.f);
     if (odd || !(s <= 3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
