@@ -287,8 +287,8 @@ typedef struct {
  *     INT4 with zero     : over the group and 0, scale = (max - min) / 15, zero = round(-min / scale), q = zero + round(w / scale).
  *     FP4                : scale = max|w| / 6, q the nearest E2M1 float to w / scale, halfway to the even code.
  *   Scales are rounded to four significant bits (to nearest; with a zero point upwards), so that a weight read back is a
- *   bf16 or fp16 number without rounding.  Codes are kept in range, in fp16 also so that no weight reads back as an infinity; a
- *   group whose scale is 0 reads back as 0, one that holds an infinity or NaN has scale NaN and reads back as NaN.
+ *   bf16 or fp16 number without rounding.  Codes (and FP4's scales) are kept where no finite weight reads back as an
+ *   infinity; a group whose scale is 0 reads back as 0, one that holds an infinity or NaN has scale NaN and reads back as NaN.
  * dora_dequantize : W [d_out, d_in] `dtype` out, rounded once.
  * r and tokens of desc are not read.  Neither needs a workspace.
  */

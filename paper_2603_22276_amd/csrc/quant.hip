@@ -113,8 +113,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
         s = four_bits_up((wide ? 0.5f * hi - 0.5f * lo : span) / 15.f);
         if (wide) s += s;
     } else s = four_bits(fmaxf(hi, -lo) / (CODE == DORA_QUANT_INT4 ? 7.f : 6.f));
-    // What is read back stays finite in fp16: 6 x 10240 is, and a code is not taken past 65504.
-    if constexpr (std::is_same<T, f16_t>::value && CODE == DORA_QUANT_FP4) s = fminf(s, 10240.f);
+    // What is read back stays finite: six times the largest number of four bits that allows it, and no code past the largest weight.
+    constexpr float largest_weight = std::is_same<T, f16_t>::value ? 65504.f : std::is_same<T, bf16_t>::value ? 0x1.fep127f : 0x1.fffffep127f;
+    if constexpr (CODE == DORA_QUANT_FP4) s = fminf(s, std::is_same<T, f16_t>::value ? 0x1.4p13f : 0x1.4p125f);
     if (odd || !(s <= 3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
     const int64_t at = (int64_t)row * p.groups + g;
     const bool first = (threadIdx.x & (lanes - 1)) == 0;
@@ -129,7 +130,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
     const bool tiny = !std::is_same<T, f16_t>::value && some && s < 0x1p-100f;
     const float by = tiny ? s * 0x1p100f : s, inv = some ? 1.f / by : 0.f;
     auto over_s = [&](float v) { const float t = v * inv; return fmaf(fmaf(-t, by, v), inv, t); };
-    const float most = std::is_same<T, f16_t>::value && some ? floorf(over_s(65504.f)) : 15.f;
+    // (bf16, fp32: only scales near the largest come so far, and others' quotients might pass it)
+    const float most = some && (std::is_same<T, f16_t>::value || s > 0x1p100f) ? floorf(over_s(largest_weight)) : 15.f;
     if constexpr (ZERO) z = some ? fminf(fmaxf(rintf(over_s(tiny ? -lo * 0x1p100f : -lo)), 0.f), 15.f) : 0.f;
     if (first) {
         V::put(p.scale, at, s);

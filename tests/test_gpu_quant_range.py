@@ -5,7 +5,7 @@ import pytest
 
 import quant_util as U
 from oracle import quant_oracle as Q
-from test_gpu_quant import quantize_on_gpu
+from test_gpu_quant import KINDS, quantize_on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +36,23 @@ def test_a_span_past_the_largest_float(dtype, group):
     W[2, ::32], W[2, 7::32] = -2.0 ** 127, 2.0 ** 127       # (the span is 2^128)
     W[3] = U.stored(np.random.default_rng(4).standard_normal(1024), "bf16")
     check(W, dtype, "zero", group, np.inf)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("group", [32, 1024])
+def test_the_largest_weights_read_back_finite(dtype, kind, group):
+    # (16-bit weights in fp32 too, as above; beside them the largest float itself)
+    M = LARGEST["bf16" if dtype == "f32" else dtype]
+    stored = lambda a: U.stored(a, "bf16" if dtype == "f32" else dtype)  # noqa: E731
+    W = stored(np.random.default_rng(5).uniform(-1, 1, (16, 1024)) * M)
+    W[0], W[1] = M, -M
+    W[2, ::32], W[2, 1::32] = -M, M
+    W[3:8] = stored(np.random.default_rng(6).uniform(0, 1, (5, 1024)) * M)
+    for row, share in zip(range(3, 8), (0.05, 0.1, 0.15, 0.2, 0.3)):
+        W[row, ::32], W[row, 1::32] = M, stored(-share * M)
+        W[row + 5] = -W[row]
+    W[13, 4:] = 0.0
+    if dtype == "f32":
+        W[14] = LARGEST["f32"]
+    check(W, dtype, kind, group, LARGEST[dtype])
