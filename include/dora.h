@@ -290,7 +290,7 @@ typedef struct {
  *   bf16 or fp16 number without rounding.  Codes (and FP4's scales) are kept where no finite weight reads back as an
  *   infinity; a group whose scale is 0 reads back as 0, one that holds an infinity or NaN has scale NaN and reads back as NaN.
  * dora_dequantize : W [d_out, d_in] `dtype` out, rounded once.
- * r and tokens of desc are not read.  Neither needs a workspace.
+ * r, tokens, s and eps of desc are not read.  Neither needs a workspace.
  */
 dora_status dora_quantize(const dora_desc* desc, const void* W, int code, int group, void* q, void* scale, void* zero, void* stream);
 dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W, void* stream);
@@ -330,7 +330,7 @@ dora_status dora_backward_quant(const dora_desc* desc, const void* dy, const voi
  * offset of t d_in / 8.
  *   p : 0 <= p < 1 (DORA_ERR_SHAPE otherwise).   counter : device, one uint64, or NULL (0): read when the launch runs, so
  *   that a captured graph draws anew in every replay.
- * What is dropped does not reach the result (NaN and infinities included).  d_out and r of desc are not read.  No workspace.
+ * What is dropped does not reach the result (NaN and infinities included).  d_out, r, s and eps of desc are not read.  No workspace.
  */
 dora_status dora_dropout(const dora_desc* desc, const void* x, double p, uint64_t seed, uint64_t offset, const uint64_t* counter,
                          void* x_lora, void* stream);

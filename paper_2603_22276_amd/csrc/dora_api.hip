@@ -145,11 +145,13 @@ struct Bump {
 constexpr int TILE = 128;
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// A 4-bit weight's struct against the desc's shape (d_out and d_in only)
+// A 4-bit weight's struct against the desc's type and shape (nothing else of it is read)
 dora_status check_quant_shape(const dora_desc* d, int code, int group, const void* zero)
 {
-    const dora_status st = check_desc(d, false);
-    if (st != DORA_OK) return st;
+    if (!d) return DORA_ERR_NULL;
+    if (d->dtype != DORA_F32 && d->dtype != DORA_BF16 && d->dtype != DORA_F16) return DORA_ERR_DTYPE;
+    const int64_t mult = is16(d->dtype) ? 8 : 4;
+    if (d->d_out < mult || d->d_out % mult) return DORA_ERR_SHAPE;
     if (d->d_in < 8 || d->d_in % 8 || d->d_out * d->d_in >= MAX_ELEMS) return DORA_ERR_SHAPE;
     if (code != DORA_QUANT_INT4 && code != DORA_QUANT_FP4) return DORA_ERR_SHAPE;
     if (group < 32 || (group & (group - 1))) return DORA_ERR_SHAPE;
