@@ -94,10 +94,12 @@ dora_status check_desc(const dora_desc* d, bool need_weights)
     const int64_t mult = is16(d->dtype) ? 8 : 4;
     if (d->d_out < mult || d->d_out % mult) return DORA_ERR_SHAPE;
     if (d->tokens < 0) return DORA_ERR_SHAPE;
+    if (d->d_out >= MAX_ELEMS || d->tokens >= MAX_ELEMS) return DORA_ERR_SHAPE;   // (each by itself: their products might wrap)
     if (d->tokens * d->d_out >= MAX_ELEMS) return DORA_ERR_SHAPE;
     if (need_weights) {
         if (d->d_in < mult || d->d_in % mult) return DORA_ERR_SHAPE;
         if (d->r < mult || d->r % mult) return DORA_ERR_SHAPE;
+        if (d->d_in >= MAX_ELEMS || d->r >= MAX_ELEMS) return DORA_ERR_SHAPE;
         if (d->d_out * d->d_in >= MAX_ELEMS || d->tokens * d->d_in >= MAX_ELEMS) return DORA_ERR_SHAPE;
         if (d->r * d->d_in >= MAX_ELEMS || d->d_out * d->r >= MAX_ELEMS || d->tokens * d->r >= MAX_ELEMS)
             return DORA_ERR_SHAPE;
@@ -151,7 +153,7 @@ dora_status check_quant_shape(const dora_desc* d, int code, int group, const voi
     if (!d) return DORA_ERR_NULL;
     if (d->dtype != DORA_F32 && d->dtype != DORA_BF16 && d->dtype != DORA_F16) return DORA_ERR_DTYPE;
     const int64_t mult = is16(d->dtype) ? 8 : 4;
-    if (d->d_out < mult || d->d_out % mult) return DORA_ERR_SHAPE;
+    if (d->d_out < mult || d->d_out % mult || d->d_out >= MAX_ELEMS || d->d_in >= MAX_ELEMS) return DORA_ERR_SHAPE;
     if (d->d_in < 8 || d->d_in % 8 || d->d_out * d->d_in >= MAX_ELEMS) return DORA_ERR_SHAPE;
     if (code != DORA_QUANT_INT4 && code != DORA_QUANT_FP4) return DORA_ERR_SHAPE;
     if (group < 32 || (group & (group - 1))) return DORA_ERR_SHAPE;
