@@ -20,7 +20,7 @@ struct QuantizeArgs {
     const void* w;
     uint32_t* q;
     void *scale, *zero;
-    int d_out, d_in, group_shift, groups;
+    int d_out, d_in, group_shift, groups, lane_shift;
 };
 
 // The largest of 16-bit pairs, both halves at once, over `lanes` (a power of two from 4 on) lanes in a row.
@@ -44,12 +44,12 @@ __device__ __forceinline__ uint32_t lanes_pair_max(uint32_t v, int lanes)
     return v;
 }
 
-// A group belongs to `lanes` = min(64, group / 8) lanes of a wave, eight weights to a lane at a time; the extremes of the group
-// meet by lane exchanges, so a weight is read once (groups above 512: twice, the second time from the L2).  16-bit floats are
-// ordered as their bits are: the extremes are found two at a time, the largest positive as it is and the most negative as the largest
-// number with the sign bit; exponents of ones show infinities and NaN.  Bound: memory, and the vector instructions of rounding
-// beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us, 3.5 TB/s (65 with the extremes, the eight quotients and the
-// eight codes of a thread one by one).
+// A group belongs to `lanes` = min(64, group / 8) lanes of a wave (fewer where the row is shorter), eight weights to a lane at a time;
+// the extremes of the group meet by lane exchanges, so a weight is read once (groups above 512: twice, the second time from the L2).
+// 16-bit floats are ordered as their bits are: the extremes are found two at a time, the largest positive as it is and the most
+// negative as the largest number with the sign bit; exponents of ones show infinities and NaN.  Bound: memory, and the vector
+// instructions of rounding beside it: 14336 x 4104 in fp16 with zero points, groups of 64, 43 us, 3.5 TB/s (65 with the extremes, the
+// eight quotients and the eight codes of a thread one by one).
 //
 // Scales have four significant bits.  A symmetric code (at most 3 bits of odd part, 4 with a zero point) times such a scale
 // has 8 at most, so the weight that codes and scale stand for is a bf16 and an fp16 number without rounding, and every path
@@ -59,8 +59,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
 {
     typedef Eight<T> V;
     const int group = 1 << p.group_shift;
-    const int lane_shift = p.group_shift - 3 < 6 ? p.group_shift - 3 : 6, lanes = 1 << lane_shift;
-    const uint32_t unit = (uint32_t)(((uint64_t)blockIdx.x * 256 + threadIdx.x) >> lane_shift);
+    const int lanes = 1 << p.lane_shift;
+    const uint32_t unit = (uint32_t)(((uint64_t)blockIdx.x * 256 + threadIdx.x) >> p.lane_shift);
     const uint32_t row = unit / (uint32_t)p.groups, g = unit - row * (uint32_t)p.groups;
     if (row >= (uint32_t)p.d_out) return;              // (the lanes of a group leave together)
     const int k_first = (int)(g << p.group_shift) + (int)(threadIdx.x & (lanes - 1)) * 8;
@@ -211,10 +211,12 @@ __global__ __launch_bounds__(256) void dequantize_kernel(QuantWeight w, T* out, 
 }
 
 template <typename T>
-hipError_t quantize_t(const QuantizeArgs& a, int code, hipStream_t st)
+hipError_t quantize_t(QuantizeArgs a, int code, hipStream_t st)
 {
-    const int lane_shift = a.group_shift - 3 < 6 ? a.group_shift - 3 : 6;
-    const int64_t threads = ((int64_t)a.d_out * a.groups) << lane_shift;
+    // (no more lanes than a short row has use for: 64 to each of 2^26 rows of 8 weights would be 2^32 threads, more than a launch takes)
+    a.lane_shift = a.group_shift - 3 < 6 ? a.group_shift - 3 : 6;
+    while (a.lane_shift > 2 && a.d_in <= 4 << a.lane_shift) --a.lane_shift;
+    const int64_t threads = ((int64_t)a.d_out * a.groups) << a.lane_shift;
     const dim3 grid((unsigned)((threads + 255) / 256)), block(256);
     if (code == DORA_QUANT_FP4) quantize_kernel<T, DORA_QUANT_FP4, false><<<grid, block, 0, st>>>(a);
     else if (a.zero) quantize_kernel<T, DORA_QUANT_INT4, true><<<grid, block, 0, st>>>(a);
@@ -240,7 +242,7 @@ hipError_t launch_quantize(int dtype, const void* W, int d_out, int d_in, int co
                            hipStream_t st)
 {
     TraceScope ts(DORA_K_QUANTIZE, st);
-    const QuantizeArgs a{W, static_cast<uint32_t*>(q), scale, zero, d_out, d_in, group_shift, quant_groups(d_in, group_shift)};
+    const QuantizeArgs a{W, static_cast<uint32_t*>(q), scale, zero, d_out, d_in, group_shift, quant_groups(d_in, group_shift), 0};
     if (dtype == DORA_F32) return quantize_t<float>(a, code, st);
     return dtype == DORA_F16 ? quantize_t<f16_t>(a, code, st) : quantize_t<bf16_t>(a, code, st);
 }
