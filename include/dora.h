@@ -71,7 +71,9 @@ typedef enum {
     DORA_PHASE_BACKWARD_DROPOUT = 6,  /* dora_backward_dropout with everything recomputed (worst case) */
     DORA_PHASE_NORM_QUANT = 7,        /* dora_norm_quant */
     DORA_PHASE_FORWARD_QUANT = 8,     /* dora_forward_quant, worst case, an input of the adapter's own among it */
-    DORA_PHASE_BACKWARD_QUANT = 9     /* dora_backward_quant, the same */
+    DORA_PHASE_BACKWARD_QUANT = 9,    /* dora_backward_quant, the same */
+    DORA_PHASE_FORWARD_QUANT_PLAIN = 10,     /* dora_forward_quant with x_lora == NULL */
+    DORA_PHASE_FORWARD_QUANT_NORM_GIVEN = 11 /* and w_norm != NULL */
 } dora_phase;
 
 /* Scratch bytes an entry point needs for this shape.  Returns 0 for an invalid desc. */
@@ -301,11 +303,15 @@ dora_status dora_dequantize(const dora_desc* desc, const dora_quant* wq, void* W
  *   x_lora : the adapter's own input as in dora_forward_dropout / dora_backward_dropout, or NULL: the plain module (as in
  *            the forward x itself).  In dora_backward_quant with x_lora, x is not read and may be NULL, and dx_lora receives
  *            the gradient of the adapter's input; without it dx_lora is not written.
- * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  In 16 bits the norm (s != 0, r <= 384,
- * d_in a multiple of 32) and the plain forward of up to 320 tokens take the codes as they are, the latter within limits of shape; everything
- * else reads W back into the workspace in the storage type first (2 or 4 bytes a weight).  Either way a product sees each weight
- * rounded at most once, which scales of up to four significant bits and zero points of 0 to 15 do not show.  An infinity in a
- * row of x makes that row of y infinite or NaN.
+ * Workspace: DORA_PHASE_NORM_QUANT, DORA_PHASE_FORWARD_QUANT, DORA_PHASE_BACKWARD_QUANT.  The last two hold room for W in the
+ * storage type whatever the call.  DORA_PHASE_FORWARD_QUANT_PLAIN (x_lora is NULL or x) and DORA_PHASE_FORWARD_QUANT_NORM_GIVEN (and
+ * w_norm is given, as a server keeps it) hold it only where such a forward may need it: for fp32, from 33 tokens on, or for a norm
+ * that is not formed from codes.
+ * In 16 bits the norm (s != 0, r <= 384, d_in a multiple of 32) and the plain forward of up to 320 tokens take the codes as they
+ * are, the latter from 33 tokens on where the groups of a row are eight or more and of an even number; everything else reads W back
+ * into the workspace in the storage type first (2 or 4 bytes a weight).  Either way a product sees each weight rounded at most
+ * once, which scales of up to four significant bits and zero points of 0 to 15 do not show.  An infinity in a row of x makes that
+ * row of y infinite or NaN.
  */
 dora_status dora_norm_quant(const dora_desc* desc, const dora_quant* wq, const void* A, const void* B, float* w_norm, void* ws,
                             size_t ws_bytes, void* stream);

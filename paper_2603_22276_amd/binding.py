@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdora.so")
 
 DORA_F32, DORA_BF16, DORA_F16 = 0, 1, 2
-PHASE_NORM, PHASE_FORWARD, PHASE_BACKWARD, PHASE_BACKWARD_RECOMPUTE, PHASE_COMPOSE_BACKWARD, PHASE_FORWARD_DROPOUT, PHASE_BACKWARD_DROPOUT, PHASE_NORM_QUANT, PHASE_FORWARD_QUANT, PHASE_BACKWARD_QUANT = range(10)
+PHASE_NORM, PHASE_FORWARD, PHASE_BACKWARD, PHASE_BACKWARD_RECOMPUTE, PHASE_COMPOSE_BACKWARD, PHASE_FORWARD_DROPOUT, PHASE_BACKWARD_DROPOUT, PHASE_NORM_QUANT, PHASE_FORWARD_QUANT, PHASE_BACKWARD_QUANT, PHASE_FORWARD_QUANT_PLAIN, PHASE_FORWARD_QUANT_NORM_GIVEN = range(12)
 QUANT_INT4, QUANT_FP4 = 0, 1
 K_COUNT = 25
 

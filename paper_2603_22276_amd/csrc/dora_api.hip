@@ -560,11 +560,23 @@ inline bool quant_tokens(const dora_desc* d)
 constexpr int64_t QUANT_TILE_MAX = 320;
 inline bool quant_tile(const dora_desc* d) { return is16(d->dtype) && d->tokens > 32 && d->tokens <= QUANT_TILE_MAX; }
 
+// Whether a forward over a 4-bit weight reads it back first: for its norm, or for a product that takes no codes
+inline bool quant_reads_back(const dora_desc* d, bool need_norm, bool takes_codes)
+{
+    return (need_norm && !norm_of_codes(d)) || (d->tokens > 0 && !takes_codes);
+}
+
 // h in one launch in front of such a product (project_tokens.hip), while every tile of 16 x 16 has a CU to itself and its columns take it a
 // round of loads and a quarter (us of a forward, sliced / this: 1024 x 4096, r 64, 33 tokens 26.4 / 24.5; 4096 x 4096, r 384, 128
 // tokens 41.0 / 36.0, 200 tokens, 312 tiles, 47.7 / 49.3; 3000 x 2056, r 72, 333 tokens 40.5 / 33.9; 5120 x 5120, r 128, 256 tokens 54.9 /
 // 52.8; 8192 x 8192, r 64, 64 tokens 45.0 / 47.5).
 inline bool project_tokens(const dora_desc* d) { return is16(d->dtype) && d->d_in <= 5120 && (d->tokens + 15) / 16 * ((d->r + 15) / 16) <= 256; }
+
+// bf16 takes the K-concatenated product: one rounding where base, lora and the compose pass had three, and no pass over
+// [tokens, d_out] beside the product (8192 x 8192, r 384, 8192 tokens, forward and backward: 2089 -> 2021 us; 4096 x 4096,
+// 4096 tokens, forward: 216 -> 191 us; 27648 x 5120 and back with recompute: 13.79 -> 12.93 ms).  fp16 keeps the compose
+// pass: s h is rounded to storage before the product, and fp16's exponent range does not hold s h wherever it holds h.
+inline bool forward_in_one_product(const dora_desc* d) { return d && d->dtype == DORA_BF16; }
 
 // scratch for the K slices of a [tokens, n] product over k whose N-side operand has rows of ldb
 inline size_t slice_floats(const dora_desc* d, int64_t n, int64_t k, int64_t ldb)
@@ -749,6 +761,15 @@ size_t dora_workspace_bytes(const dora_desc* desc, int phase)
         case DORA_PHASE_BACKWARD_DROPOUT: { BwdPlan p; plan_bwd(desc, b, p, true, true, true, true); break; }
         case DORA_PHASE_NORM_QUANT: { NormPlan n; if (!norm_of_codes(desc)) take_weight(desc, b); plan_norm(desc, b, n); break; }
         case DORA_PHASE_FORWARD_QUANT: { FwdPlan p; take_weight(desc, b); plan_fwd(desc, b, p, true, true, true, true, true, true); break; }
+        case DORA_PHASE_FORWARD_QUANT_PLAIN:
+        case DORA_PHASE_FORWARD_QUANT_NORM_GIVEN: {
+            // (the tiles that decode depend on the groups, which are not in desc: taken as reading back)
+            const bool need_norm = phase == DORA_PHASE_FORWARD_QUANT_PLAIN, one_product = forward_in_one_product(desc);
+            FwdPlan p;
+            if (quant_reads_back(desc, need_norm, quant_tokens(desc))) take_weight(desc, b);
+            plan_fwd(desc, b, p, need_norm, true, !one_product && is16(desc->dtype), one_product, false, true);
+            break;
+        }
         case DORA_PHASE_BACKWARD_QUANT: { BwdPlan p; take_weight(desc, b); plan_bwd(desc, b, p, true, true, true, true); break; }
         default: return 0;
     }
@@ -934,7 +955,7 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     // over 4 bits the streaming launch is the faster one wherever it runs; it takes the weight as it is
     const bool streamed = !dropout && (wq ? quant_tokens(desc) : few_tokens(desc, one_product));
     const bool tiled = wq && !dropout && quant_tile(desc) && quant_tile_takes(*wq);
-    const bool need_weight = wq && ((need_norm && !norm_of_codes(desc)) || (desc->tokens > 0 && !streamed && !tiled));
+    const bool need_weight = wq && quant_reads_back(desc, need_norm, streamed || tiled);
     if (wq && need_norm && norm_refused(desc)) return DORA_ERR_SHAPE;
     Bump sizing(nullptr);
     FwdPlan p;
@@ -1038,12 +1059,6 @@ static dora_status forward_impl(const dora_desc* desc, const void* x, const void
     DORA_HIP(launch_compose_fwd(desc->dtype, p.base_a, lora, p.g, p.gm1, bias, desc->s, y, 2, saved_inner, T, d_out, s));
     return DORA_OK;
 }
-
-// bf16 takes the K-concatenated product: one rounding where base, lora and the compose pass had three, and no pass over
-// [tokens, d_out] beside the product (8192 x 8192, r 384, 8192 tokens, forward and backward: 2089 -> 2021 us; 4096 x 4096,
-// 4096 tokens, forward: 216 -> 191 us; 27648 x 5120 and back with recompute: 13.79 -> 12.93 ms).  fp16 keeps the compose
-// pass: s h is rounded to storage before the product, and fp16's exponent range does not hold s h wherever it holds h.
-static bool forward_in_one_product(const dora_desc* d) { return d && d->dtype == DORA_BF16; }
 
 dora_status dora_forward(const dora_desc* desc, const void* x, const void* W, const void* A, const void* B,
                          const float* m, const float* w_norm, const void* bias, void* y, void* saved_h, void* saved_inner,
