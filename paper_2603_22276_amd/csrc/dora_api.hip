@@ -407,18 +407,20 @@ hipError_t contract(int dtype, bool a_kc, bool b_kc, int M, int N, const Seg* se
 
 // ------------------------------------------------------------------------------------------------
 // factored norm (Sec. 2, Algorithm 1)
-// base_sq != nullptr: the base term of Eq. 2 comes from the caller's cache and W is not squared again
-// c == nullptr: only the terms are wanted.  terms != nullptr: [3, d_out] fp32 receives base_sq, cross, ba_sq.
-// G_out != nullptr: [r, r] fp32 receives the Gram matrix of Eq. 4.
-// waiting != nullptr: the last launch may be left there.
-// G is an operand of the B G product (16-bit): a rank whose Gram matrix cannot be one
+
 // The norm of a 4-bit weight whose sums come from the codes (norm_quant.hip): rows of codes in 16-byte pieces.  Elsewhere the norm
 // needs the weight read back.
 inline bool norm_of_codes(const dora_desc* d) { return is16(d->dtype) && d->s != 0.f && d->r <= NORM_ROWS_MAX_RANK && d->d_in % 32 == 0; }
+// G is an operand of the B G product (16-bit): a rank whose Gram matrix cannot be one
 inline bool norm_refused(const dora_desc* d) { return is16(d->dtype) && d->s != 0.f && d->r * d->r >= MAX_ELEMS; }
 // Eq. 6 riding on the norm's last launch: set `done` when g / gm1 were written there
 struct MagOut { const float* m; float eps; float* g; float* gm1; bool done; };
 
+// base_sq != nullptr: the base term of Eq. 2 comes from the caller's cache and W is not squared again
+// c == nullptr: only the terms are wanted.  terms != nullptr: [3, d_out] fp32 receives base_sq, cross, ba_sq.
+// G_out != nullptr: [r, r] fp32 receives the Gram matrix of Eq. 4.
+// waiting != nullptr: the last launch may be left there.
+// wq != nullptr: the weight in 4 bits, taken instead of W where norm_of_codes() says so.
 dora_status norm_impl(const dora_desc* d, const void* W, const void* A, const void* B, float* c, const NormPlan& n,
                       hipStream_t st, const float* base_sq = nullptr, float* terms = nullptr, float* G_out = nullptr,
                       MagOut* mag = nullptr, Waiting* waiting = nullptr, const QuantWeight* wq = nullptr)
@@ -554,9 +556,14 @@ inline bool quant_tokens(const dora_desc* d)
     return is16(d->dtype) && d->tokens > 0 && d->tokens <= 32 && d->tokens * d->r < (int64_t)1 << 29;
 }
 
-// and of more tokens, as long as decoding in the product costs less than reading the weight back (us, read back / decoded, weights
-// from memory, h in slices in both: 33 tokens 1024 x 4096, r 64 32 / 26, 64 tokens 14336 x 4096 89 / 49, 256 tokens 4096 x 4096 48 / 46, 8192 x 8192 91 /
-// 76, 27648 x 5120 210 / 111; 384 tokens 53 / 53 and 103 / 106 at the first two of these, 1024 tokens 63 / 78).
+// and of more tokens, as long as decoding in the product costs less than reading the weight back.  One number of tokens for all shapes
+// (us of a forward, read back / decoded, weights from memory, bf16, groups of 128, r 64, at 27648 rows 384):
+//                 33 tokens   64          128         256          320          384          512
+//   1024 x 4096    29 / 24    29 / 25     29 / 26     31 / 28      32 / 30      33 / 30      34 / 32
+//   4096 x 4096    37 / 28    37 / 30     38 / 35     45 / 41      46 / 45      47 / 48      52 / 57
+//   8192 x 8192    71 / 44    73 / 46     80 / 60     92 / 80     100 / 105    106 / 108    113 / 120
+//   14336 x 4096   62 / 37    64 / 41     69 / 52     76 / 76      95 / 85      94 / 88     105 / 98
+//   27648 x 5120  142 / 66   148 / 72    159 / 90    216 / 120    221 / 208    222 / 212    225 / 220
 constexpr int64_t QUANT_TILE_MAX = 320;
 inline bool quant_tile(const dora_desc* d) { return is16(d->dtype) && d->tokens > 32 && d->tokens <= QUANT_TILE_MAX; }
 
@@ -1241,7 +1248,9 @@ static dora_status backward_impl(const dora_desc* desc, const void* dy, const vo
         waiting.dm_args = DmFinalArgs{p.dm_partial, compose_bwd_slabs(T, d_out, dt), c, eff_eps(desc), dm, d_out};
     }
 
-    // dh = s * dz B   (gradient reaching h)
+    // dh = s * dz B   (gradient reaching h).  In 16 bits dz, dh and h are rounded once each to the storage type, as operands of 16-bit
+    // products, and inner as the tensor that a forward saves: dA and dB are 2.4e-3 of their size off in bf16 (fp16 2.9e-4), dm 1.8e-3
+    // (3.1e-4), at 4096 x 4096, r 384, 4096 tokens (3000 x 2056, r 72, 1501 tokens); the sums themselves are fp32.
     if ((dropout ? dx_lora : dx) || dA) {
         Seg sh{p.dz, d_out, B, r, d_out};
         DORA_HIP(contract(dt, true, false, T, r, &sh, 1, desc->s, p.dh, r, false, DORA_K_GEMM_DH, s, p.skp, nullptr, 0.f, &waiting));

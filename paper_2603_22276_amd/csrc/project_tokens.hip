@@ -1,7 +1,8 @@
 // h = x A^T of a few hundred tokens in one launch, in front of a product over a 4-bit weight.  An output tile of 16 tokens x 16 ranks is
 // all that a workgroup has; its sixteen waves share the columns, 64 at a time (a row's 128 bytes, two MFMA k-steps), hold their sums in
 // fp32 and add them in LDS in wave order.  Fragments come straight from memory: a wave asks for four such pieces of both operands
-// before it multiplies the first, so 4096 columns cost one latency.
+// before it multiplies the first, so 4096 columns cost one latency.  h, and s h for the K-concatenated product, are rounded once each from
+// those sums: they are operands of a 16-bit product.
 //
 // Bound: the latency of the first loads and the L1, which looks up sixteen rows for a load (16 cycles and more).  Tiles of 128 x 128 with K
 // in slices and a launch that sums them, which other sizes take, are 6.8 and 4.0 us of 4096 columns and a launch more between them.

@@ -53,7 +53,8 @@ __device__ __forceinline__ uint32_t lanes_pair_max(uint32_t v, int lanes)
 //
 // Scales have four significant bits.  A symmetric code (at most 3 bits of odd part, 4 with a zero point) times such a scale
 // has 8 at most, so the weight that codes and scale stand for is a bf16 and an fp16 number without rounding, and every path
-// (streamed, tiled, backward) multiplies with the same one.  The step grows by up to 1/16 for it.
+// (streamed, tiled, backward) multiplies with the same one.  The step grows by up to 1/16 for it.  In fp32 the same, so that codes and
+// scales of a weight serve a module of any storage type.
 template <typename T, int CODE, bool ZERO>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs p)
 {

@@ -1,5 +1,6 @@
 // Forward of a batch over a 4-bit weight where reading the weight back first would cost more than decoding it in the product:
-//   y = g (.) (x W^T + s h B^T) (+ bias), h = x A^T there already.
+//   y = g (.) (x W^T + s h B^T) (+ bias), h = x A^T there already, rounded once to the storage type: it is the operand of a 16-bit
+// product, and the tensor that a backward is given.
 //
 // A workgroup owns a tile of rows of W and of tokens.  Steps of 128 columns go through three LDS stages filled by direct loads
 // (codes as they are, a quarter of the bytes of a 16-bit weight; x in 16 bits), the low-rank part through the same stages, 64 ranks
@@ -9,8 +10,8 @@
 // gives for all rows.
 //
 // Bound: reading the codes up to about 64 tokens, beyond by issuing: a wave's 80 MFMAs of a step (16 of them for the sums of x) and the
-// 300 vector instructions of decoding and scaling its rows share one port.  8192 x 8192, r 64, 256 tokens 76 us (91 with the weight
-// read back first), 64 tokens 14336 x 4096 49 us (89).
+// 300 vector instructions of decoding and scaling its rows share one port.  A forward with weights from memory: 8192 x 8192, r 64, 256
+// tokens 80 us (92 with the weight read back first), 14336 x 4096, 64 tokens 41 us (64).
 #include "quant_codes.hpp"
 
 namespace dora {
@@ -392,8 +393,8 @@ constexpr int SMALL_TOK = 64, SMALL_ROWS = 128, LARGE_TOK = 128, LARGE_ROWS = 25
 // workgroup has a CU to itself and 17 where two share one, of a large tile 24 (four times the products), 60 for what comes before the
 // first step and behind the last; and where there are slices 40 for the launch that sums them, and the partial sums written and read at
 // 4 TB/s.  At most eight slices of four steps at least.  Groups of 32: small tiles (the large one's scales and codes do not fit the
-// registers).  (Forward, us, small / large: 4096 x 4096, r 64, 128 tokens 40.0 / 49.4; 14336 x 4096, 128 tokens 60.3 / 56.1; 8192 x
-// 8192, 256 tokens 88.9 / 77.7; 27648 x 5120, 256 tokens 158 / 112.)
+// registers).  (Forward, h in slices in both, us, small / large: 4096 x 4096, r 64, 128 tokens 40.0 / 49.4; 14336 x 4096, 128 tokens
+// 60.3 / 56.1; 8192 x 8192, 256 tokens 88.9 / 77.7; 27648 x 5120, 256 tokens 158 / 112.)
 struct Choice { bool small; int slices; };
 Choice choose(int64_t tokens, int64_t d_out, int64_t d_in, int group_shift)
 {
